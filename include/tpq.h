@@ -332,6 +332,119 @@ int tpq_decode_reduce_static(const tpq_layout *L, const void *plan, int n_ranks,
                              const float *step, int accum, int out_dtype, void *out,
                              int64_t ldOut, void *stream);
 
+/* ---- keys and values in 4 bits: a paged cache and the attention over it -----------------
+ * What an attention block does between its projections at serving time, on one device with
+ * its share of the heads; the attention's output is the X of the block's row-parallel linear
+ * layer (tpq_gemm_encode).  Keys and values are held in this library's 4-bit form, quantised
+ * per token, head and group of G features exactly as tpq_encode does it (zero, scale in
+ * bf16, codes 0..15, x_hat = code * scale + zero).
+ *
+ * The cache [device] is the caller's buffer of n_pages pages of L.page_bytes; a page holds
+ * `page` tokens of every key/value head, head h's cell (L.cell_bytes) at h * cell_bytes:
+ *     K codes [page][D/2] bytes  dword g*D/32 + kk of a row (g < 4, kk < D/32): features
+ *                                32kk + 8g + 0..7, feature 2t of them in bits 4t, feature
+ *                                2t + 1 in bits 16 + 4t
+ *     V codes [page][D/2] bytes  chunk m < 16 of D/32 bytes: feature 16n + m in bits 4n
+ *     K meta  [ng][page]         scale (lower half) and zero (upper half) of a group, bf16
+ *     V meta  [ng][page]
+ * It needs no initialisation.  A batch says where its sequences' tokens lie:
+ *     table  [device] int32 [n_seqs][ld_table]: page numbers; token j of sequence b is token
+ *            j % page of page table[b][j / page].  Sequences may share pages that none of them
+ *            appends to.  Entries past a sequence's last token are not read as pages.
+ *     lens   [device] int32 [n_seqs]: tokens in the cache, the batch's new ones included
+ *     starts [device] int32 [n_seqs + 1] or NULL: rows starts[b] .. starts[b+1] - 1 of the
+ *            batch's matrices are sequence b's new tokens, its last ones: row i of n is at
+ *            position lens[b] - n + i.  NULL: row b is sequence b's one new token (rows >= n_seqs)
+ *     max_new  no sequence has more new tokens (those past it are left out)
+ *     max_len  a hint: no sequence is expected to be longer (how the work is split goes by it;
+ *              a longer sequence costs time only); at most ld_table * page
+ *     rows     rows of the batch's matrices; those behind the last sequence are neither read
+ *              nor written
+ * Everything on the device may change between calls (and replays of a captured call) within
+ * these host numbers.  Nothing outside the buffers is ever touched: a sequence whose starts lie
+ * outside 0..rows or decrease is left out, a token whose page number is outside 0..n_pages - 1, or
+ * whose position is outside the table, counts as absent: not written, not read, not seen.
+ * tpq_kv_check reports all of these. */
+#define TPQ_KV_MAX_HEADS 256
+
+typedef struct tpq_kv_layout {
+    int32_t heads;      /* key/value heads on this device, 1 .. TPQ_KV_MAX_HEADS        */
+    int32_t D;          /* features per head: 64, 128 or 256                            */
+    int32_t G;          /* quantisation group: 32, 64, 128 or 256, at most D            */
+    int32_t page;       /* tokens per page: 16, 32, 64, 128 or 256                      */
+    int32_t ng;         /* D / G                                                        */
+    int32_t reserved;
+    int64_t cell_bytes; /* page * (D + 8 ng)                                            */
+    int64_t page_bytes; /* heads * cell_bytes                                           */
+} tpq_kv_layout;
+
+typedef struct tpq_kv_batch {
+    const int32_t *table;
+    const int32_t *lens;
+    const int32_t *starts;
+    int32_t n_seqs;   /* 1 .. 65535                                                     */
+    int32_t ld_table; /* entries per row of the table; ld_table * page <= 2^28          */
+    int32_t max_new;  /* 1 .. 2^20; 1 where starts is NULL                              */
+    int32_t max_len;  /* 1 .. ld_table * page                                           */
+    int64_t rows;
+    int64_t n_pages;
+} tpq_kv_batch;
+
+/* [host] Derive the layout.  TPQ_ERR_UNSUPPORTED: another D, G or page; TPQ_ERR_SHAPE: heads. */
+int tpq_kv_layout_init(tpq_kv_layout *L, int heads, int D, int G, int page);
+
+/* Synchronises the stream and looks the batch over: TPQ_ERR_INDEX for starts that decrease or leave
+ * 0..rows, more than max_new new tokens, more new tokens than tokens, a length below 0 or past the
+ * table, a page number outside 0..n_pages - 1 among the used ones. */
+int tpq_kv_check(const tpq_kv_layout *L, const tpq_kv_batch *batch, void *stream);
+
+/* New tokens into the cache: K and V quantised, K (and the queries Q, if given) rotated by
+ * their positions first.
+ *     K, V   [device] bf16 [rows][ldK], [rows][ldV]: head h's features at h * D; may be parts of
+ *            one wider matrix
+ *     Q      [device] bf16 [rows][ldQ], q_heads heads of D, or NULL; Q_out [device] bf16 [rows][ldQo]
+ *            receives them rotated (Q_out = Q with ldQo = ldQ: in place)
+ *     rot_cos, rot_sin [device] fp32 [rot_rows][rot / 2]: entry p of position pos turns pair p of
+ *            each head: (x0, x1) -> (bf16(x0 c - x1 s), bf16(x1 c + x0 s)), products and sum each
+ *            rounded to fp32.  rot_mode TPQ_ROT_HALVES: pair p is features p and p + rot/2;
+ *            TPQ_ROT_PAIRS: features 2p and 2p + 1.  Features from rot on stay as they are.
+ *     rot    a multiple of 16, 0 (no rotation: the tables may be NULL) .. D
+ * Tokens at positions from rot_rows on are left out (rot > 0).  ld*: elements, multiples of 8. */
+#define TPQ_ROT_HALVES 0
+#define TPQ_ROT_PAIRS 1
+int tpq_kv_append(const tpq_kv_layout *L, void *cache, const tpq_kv_batch *batch,
+                  const uint16_t *K, int64_t ldK, const uint16_t *V, int64_t ldV,
+                  const float *rot_cos, const float *rot_sin, int rot, int rot_rows, int rot_mode,
+                  const uint16_t *Q, int64_t ldQ, int q_heads, uint16_t *Q_out, int64_t ldQo, void *stream);
+
+/* The cache's values of the batch's new tokens (with starts that cover whole sequences: of all of
+ * their tokens), dequantised: what tpq_kv_append's rows have become, for another device or format.
+ *     K_out, V_out [device] fp32 or bf16 (out_dtype; bf16: rounded once) [rows][ldK], [rows][ldV],
+ *            either may be NULL; ld*: elements, multiples of 4 (fp32) or 8 (bf16)
+ * Rows of absent tokens are left as they are. */
+int tpq_kv_read(const tpq_kv_layout *L, const void *cache, const tpq_kv_batch *batch, int out_dtype,
+                void *K_out, int64_t ldK, void *V_out, int64_t ldV, void *stream);
+
+/* Attention of the batch's new tokens over the cache (which holds them already).  Query head
+ * hq of q_heads (a multiple of L.heads) goes with key/value head hq / (q_heads / L.heads).  The
+ * token at position p sees key j iff j <= p and (window = 0 or j > p - window or j < sinks):
+ *     s_j = scale * q . k_j;  softcap > 0: s_j = softcap * tanh(s_j / softcap)
+ *     out = sum_j exp(s_j) v_j / sum_j exp(s_j)        over the keys it sees; none: 0
+ * with k_j, v_j the cache's values.  Scores, exponentials' sums and accumulators are fp32.
+ * With up to 32 rows of a head (new tokens * q_heads / L.heads) per sequence the products take the
+ * codes themselves, which are exact in bf16, and the probabilities as pairs of bf16 (17 bits);
+ * with more, keys and values are rounded to fp16 at a scale of their own and so are the probabilities (2^-12).
+ *     Q, out    [device] bf16 [rows][ldQ], [rows][ldOut], elements, multiples of 8
+ *     window, sinks  >= 0, at most 2^28 (sinks without a window change nothing)
+ *     workspace [device] >= tpq_kv_attention_workspace_bytes(..) bytes (which depends on L, the batch's
+ *               host numbers, q_heads and the current device's compute units), 16-byte aligned,
+ *               contents arbitrary; calls that share a workspace must not overlap in time */
+size_t tpq_kv_attention_workspace_bytes(const tpq_kv_layout *L, const tpq_kv_batch *batch, int q_heads);
+int tpq_kv_attention(const tpq_kv_layout *L, const void *cache, const tpq_kv_batch *batch,
+                     const uint16_t *Q, int64_t ldQ, int q_heads, float scale, int window, int sinks,
+                     float softcap, uint16_t *out, int64_t ldOut, void *workspace, size_t ws_bytes,
+                     void *stream);
+
 #ifdef __cplusplus
 }
 #endif

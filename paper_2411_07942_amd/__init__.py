@@ -37,6 +37,7 @@ EXPORTS = [
     "tpq_calibrate_finalize_workspace_bytes", "tpq_calibrate_finalize",
     "tpq_encode", "tpq_hop", "tpq_gemm_weights", "tpq_gemm_encode", "tpq_decode_reduce", "tpq_decode_reduce_fused",
     "tpq_static_table_floats", "tpq_static_params", "tpq_encode_static", "tpq_decode_reduce_static",
+    "tpq_kv_layout_init", "tpq_kv_check", "tpq_kv_append", "tpq_kv_read", "tpq_kv_attention_workspace_bytes", "tpq_kv_attention",
 ]
 
 
@@ -47,6 +48,21 @@ class Layout(ctypes.Structure):
                 ("code_bytes", ctypes.c_int32), ("reserved", ctypes.c_int32),
                 ("pitch_codes", ctypes.c_int64), ("pitch_meta", ctypes.c_int64),
                 ("pitch_outl", ctypes.c_int64), ("wire_bytes_per_row", ctypes.c_int64)]
+
+
+class KvLayout(ctypes.Structure):
+    """Mirror of ``tpq_kv_layout``."""
+    _fields_ = [("heads", ctypes.c_int32), ("D", ctypes.c_int32), ("G", ctypes.c_int32), ("page", ctypes.c_int32),
+                ("ng", ctypes.c_int32), ("reserved", ctypes.c_int32),
+                ("cell_bytes", ctypes.c_int64), ("page_bytes", ctypes.c_int64)]
+
+
+class _KvBatch(ctypes.Structure):
+    """Mirror of ``tpq_kv_batch`` (rows and n_pages are the calls' to fill in), and the device its tensors are on."""
+    _fields_ = [("table", ctypes.c_void_p), ("lens", ctypes.c_void_p), ("starts", ctypes.c_void_p),
+                ("n_seqs", ctypes.c_int32), ("ld_table", ctypes.c_int32), ("max_new", ctypes.c_int32),
+                ("max_len", ctypes.c_int32), ("rows", ctypes.c_int64), ("n_pages", ctypes.c_int64),
+                ("device", ctypes.c_int32)]
 
 
 class TpqError(RuntimeError):
@@ -104,6 +120,15 @@ def _load():
     lib.tpq_static_params.argtypes = [LP, vp, vp, vp, c_int, vp, vp, vp]
     lib.tpq_encode_static.argtypes = [LP, vp, vp, i64, c_int, i64, vp, vp, vp, vp]
     lib.tpq_decode_reduce_static.argtypes = [LP, vp, c_int, i64, vp, vp, vp, c_int, c_int, vp, i64, vp]
+    KP, BP = ctypes.POINTER(KvLayout), ctypes.POINTER(_KvBatch)
+    lib.tpq_kv_layout_init.argtypes = [KP, c_int, c_int, c_int, c_int]
+    lib.tpq_kv_check.argtypes = [KP, BP, vp]
+    lib.tpq_kv_append.argtypes = [KP, vp, BP, vp, i64, vp, i64, vp, vp, c_int, c_int, c_int, vp, i64, c_int, vp, i64, vp]
+    lib.tpq_kv_read.argtypes = [KP, vp, BP, c_int, vp, i64, vp, i64, vp]
+    lib.tpq_kv_attention_workspace_bytes.argtypes = [KP, BP, c_int]
+    lib.tpq_kv_attention_workspace_bytes.restype = sz
+    lib.tpq_kv_attention.argtypes = [KP, vp, BP, vp, i64, c_int, ctypes.c_float, c_int, c_int, ctypes.c_float, vp, i64,
+                                     vp, sz, vp]
     _lib = lib
     return lib
 
@@ -388,3 +413,104 @@ def decode_reduce_static_call(L: Layout, plan: torch.Tensor, msgs: Sequence[Mess
 
 def decode_reduce_static(L, plan, msgs, step, out, accum: int = ACC_FP32, stream=None) -> None:
     _native().decode_reduce_static(L, plan, msgs, step, out, accum, stream)
+
+
+# ---- keys and values in 4 bits: a paged cache and the attention over it --------------------------
+
+def kv_layout_init(heads: int, D: int, G: int, page: int) -> KvLayout:
+    L = KvLayout()
+    _check(_load().tpq_kv_layout_init(ctypes.byref(L), heads, D, G, page), "tpq_kv_layout_init")
+    return L
+
+
+def kv_cache(L: KvLayout, n_pages: int, device) -> torch.Tensor:
+    """A cache of n_pages pages (any uint8 buffer of n_pages * L.page_bytes will do; its contents do not matter)."""
+    return torch.empty(n_pages * L.page_bytes, dtype=torch.uint8, device=device)
+
+
+class KvBatch:
+    """Where a batch's sequences lie (tpq_kv_batch): table int32 [n_seqs, entries], page numbers; lens int32
+    [n_seqs], tokens in the cache with the new ones; starts int32 [n_seqs + 1], the rows of each sequence's new tokens, or
+    None: one new token per sequence, row b for sequence b.  max_new: no sequence has more new tokens; max_len: no
+    sequence is expected to be longer (None: the whole table).  The tensors are read at each call, on the device."""
+
+    def __init__(self, table: torch.Tensor, lens: torch.Tensor, starts: Optional[torch.Tensor] = None, max_new: int = 1,
+                 max_len: Optional[int] = None):
+        n = table.shape[0] if table.dim() == 2 else -1
+        for t in (table, lens) if starts is None else (table, lens, starts):
+            if t.dtype != torch.int32 or t.device != table.device or not t.is_cuda:
+                raise AssertionError("table, lens and starts are int32 tensors on one GPU")
+        if n < 1 or table.shape[1] < 1 or not table.is_contiguous():
+            raise AssertionError("table is a contiguous [n_seqs, entries]")
+        if lens.shape != (n,) or not lens.is_contiguous():
+            raise AssertionError("lens is a contiguous [n_seqs]")
+        if starts is not None and (starts.shape != (n + 1,) or not starts.is_contiguous()):
+            raise AssertionError("starts is a contiguous [n_seqs + 1]")
+        if max_new < 1 or (max_len is not None and max_len < 1):
+            raise AssertionError("max_new and max_len are at least 1")
+        self.table, self.lens, self.starts = table, lens, starts
+        self.max_new, self.max_len = int(max_new), max_len
+        self._c = _KvBatch(table.data_ptr(), lens.data_ptr(), None if starts is None else starts.data_ptr(), n,
+                           table.shape[1], int(max_new), 0 if max_len is None else int(max_len), 0, 0, table.device.index)
+
+    def _for(self, L: KvLayout, rows: int, n_pages: int) -> _KvBatch:
+        c = _KvBatch.from_buffer_copy(self._c)
+        c.rows, c.n_pages = rows, n_pages
+        c.max_len = c.max_len or min(c.ld_table * L.page, 0x7FFFFFFF)
+        return c
+
+
+def kv_check(L: KvLayout, cache: torch.Tensor, batch: KvBatch, rows: int, stream=None) -> None:
+    """Waits for the stream and raises where the batch (whose matrices have `rows` rows) does not fit (tpq_kv_check)."""
+    c = batch._for(L, rows, cache.numel() * cache.element_size() // L.page_bytes)
+    _check(_load().tpq_kv_check(ctypes.byref(L), ctypes.byref(c), _stream(stream)), "tpq_kv_check")
+
+
+def kv_append_call(L: KvLayout, cache: torch.Tensor, batch: KvBatch, K: torch.Tensor, V: torch.Tensor,
+                   cos: Optional[torch.Tensor] = None, sin: Optional[torch.Tensor] = None, pairs: bool = False,
+                   Q: Optional[torch.Tensor] = None, Q_out: Optional[torch.Tensor] = None):
+    """Marshal a tpq_kv_append call once; the returned function(stream=None) issues it."""
+    return _native().kv_append_call(L, cache, batch, K, V, cos, sin, pairs, Q, Q_out)
+
+
+def kv_append(L: KvLayout, cache: torch.Tensor, batch: KvBatch, K: torch.Tensor, V: torch.Tensor,
+              cos: Optional[torch.Tensor] = None, sin: Optional[torch.Tensor] = None, pairs: bool = False,
+              Q: Optional[torch.Tensor] = None, Q_out: Optional[torch.Tensor] = None, stream=None) -> None:
+    """The batch's new tokens into the cache: K, V bf16 [rows, heads, D] (parts of a wider matrix will do), K and Q
+    (bf16 [rows, q_heads, D]; into Q_out, None: in place) turned by cos, sin (fp32 [positions, rotated features / 2])."""
+    _native().kv_append(L, cache, batch, K, V, cos, sin, pairs, Q, Q_out, stream)
+
+
+def kv_read_call(L: KvLayout, cache: torch.Tensor, batch: KvBatch, K_out: Optional[torch.Tensor],
+                 V_out: Optional[torch.Tensor]):
+    """Marshal a tpq_kv_read call once; the returned function(stream=None) issues it."""
+    return _native().kv_read_call(L, cache, batch, K_out, V_out)
+
+
+def kv_read(L: KvLayout, cache: torch.Tensor, batch: KvBatch, K_out: Optional[torch.Tensor],
+            V_out: Optional[torch.Tensor], stream=None) -> None:
+    """The cache's values of the batch's new tokens into K_out, V_out (fp32 or bf16 [rows, heads, D])."""
+    _native().kv_read(L, cache, batch, K_out, V_out, stream)
+
+
+def kv_attention_workspace_bytes(L: KvLayout, batch: KvBatch, q_heads: int) -> int:
+    c = batch._for(L, batch._c.n_seqs, 1)
+    return int(_load().tpq_kv_attention_workspace_bytes(ctypes.byref(L), ctypes.byref(c), q_heads))
+
+
+def kv_attention_workspace(L: KvLayout, batch: KvBatch, q_heads: int, device) -> torch.Tensor:
+    """A workspace for kv_attention(): for this batch's numbers and q_heads query heads."""
+    return torch.empty(max(kv_attention_workspace_bytes(L, batch, q_heads), 16), dtype=torch.uint8, device=device)
+
+
+def kv_attention_call(L: KvLayout, cache: torch.Tensor, batch: KvBatch, Q: torch.Tensor, out: torch.Tensor, scale: float,
+                      workspace: torch.Tensor, window: int = 0, sinks: int = 0, softcap: float = 0.0):
+    """Marshal a tpq_kv_attention call once; the returned function(stream=None) issues it."""
+    return _native().kv_attention_call(L, cache, batch, Q, out, scale, workspace, window, sinks, softcap)
+
+
+def kv_attention(L: KvLayout, cache: torch.Tensor, batch: KvBatch, Q: torch.Tensor, out: torch.Tensor, scale: float,
+                 workspace: torch.Tensor, window: int = 0, sinks: int = 0, softcap: float = 0.0, stream=None) -> None:
+    """out = softmax(scale * Q K^T) V of the batch's new tokens over the cache; Q, out bf16 [rows, q_heads, D].  A token
+    sees the keys up to its own, of those (window > 0) the last `window` and the first `sinks`."""
+    _native().kv_attention(L, cache, batch, Q, out, scale, workspace, window, sinks, softcap, stream)

@@ -24,7 +24,7 @@ namespace {
 PyObject *g_check;         // Python: raises TpqError for a code that is not TPQ_OK
 PyObject *g_get_device;    // torch._C._cuda_getDevice
 PyObject *g_get_stream;    // torch._C._cuda_getCurrentRawStream
-PyObject *s_codes, *s_scale, *s_zero, *s_outl, *s_cuda_stream, *s_stream, *s_data_ptr;
+PyObject *s_codes, *s_scale, *s_zero, *s_outl, *s_cuda_stream, *s_stream, *s_data_ptr, *s_c;
 
 // ---- at the boundary to C ------------------------------------------------------------------
 
@@ -253,6 +253,64 @@ struct Layout {  // the ctypes structure, by reference
     }
 };
 
+// The ctypes structures of the 4-bit cache: its layout, and a KvBatch's (whose rows and pages the calls fill in).
+struct KvBatch {
+    tpq_kv_batch b;
+    int32_t device;  // of its tensors
+};
+template <typename T>
+bool kv_struct(PyObject *o, const char *what, T &to)
+{
+    Py_buffer view;
+    if (PyObject_GetBuffer(o, &view, PyBUF_SIMPLE) != 0) return false;
+    const bool fits = view.len == static_cast<Py_ssize_t>(sizeof(T));
+    if (fits) memcpy(&to, view.buf, sizeof(T));
+    PyBuffer_Release(&view);
+    if (!fits) PyErr_Format(PyExc_TypeError, "a %s is expected", what);
+    return fits;
+}
+
+bool current_device(int &dev)
+{
+    const Ref o(PyObject_CallNoArgs(g_get_device));
+    if (!o.p) return false;
+    dev = static_cast<int>(PyLong_AsLong(o.p));
+    return !(dev == -1 && PyErr_Occurred());
+}
+
+// A tensor of the current device (the stream and the kernels are that device's), and its address.
+const at::Tensor *tensor_here(PyObject *o, int dev, void *&p)
+{
+    const at::Tensor *t = tensor(o);
+    if (!t) return nullptr;
+    if (!t->is_cuda() || t->get_device() != dev) {
+        failed_check("every tensor is on the current device");
+        return nullptr;
+    }
+    return pointer(o, p) ? t : nullptr;
+}
+
+// [rows, heads, D] or [rows, heads * D], a row's heads side by side (any row stride); heads = 0: as many as there are
+bool head_rows(PyObject *o, int dev, const char *what, int64_t D, int64_t &heads, int64_t &rows, at::ScalarType type, void *&p, int64_t &ld)
+{
+    const at::Tensor *t = tensor_here(o, dev, p);
+    if (!t) return false;
+    bool ok = t->scalar_type() == type && (t->dim() == 2 || t->dim() == 3);
+    if (ok) {
+        const int64_t last = t->dim() - 1, n = t->dim() == 3 ? t->size(1) : t->size(1) / D;
+        ok = t->size(last) == (t->dim() == 3 ? D : n * D) && t->stride(last) == 1 && (t->dim() == 2 || n <= 1 || t->stride(1) == D) &&
+             (heads == 0 || heads == n) && (rows < 0 || rows == t->size(0));
+        heads = n;
+        rows = t->size(0);
+    }
+    if (!ok) {
+        PyErr_Format(PyExc_AssertionError, "%s", what);
+        return false;
+    }
+    ld = rows > 1 ? t->stride(0) : heads * D;  // (what a single row's stride says does not matter)
+    return true;
+}
+
 bool check(int rc, const char *where)
 {
     if (rc == TPQ_OK) return true;
@@ -264,9 +322,9 @@ bool check(int rc, const char *where)
 
 // ---- the calls that can be marshalled once and issued many times -------------------------
 
-enum Kind { kEncode, kHop, kGemm, kDecode, kFused, kEncodeStatic, kDecodeStatic };
+enum Kind { kEncode, kHop, kGemm, kDecode, kFused, kEncodeStatic, kDecodeStatic, kKvAppend, kKvRead, kKvAttend };
 
-constexpr Py_ssize_t kArgs[] = {4, 6, 5, 5, 7, 5, 6}, kMaxArgs = 7;
+constexpr Py_ssize_t kArgs[] = {4, 6, 5, 5, 7, 5, 6, 10, 5, 10}, kMaxArgs = 10;
 
 struct Call {
     Kind kind;
@@ -277,6 +335,14 @@ struct Call {
     int n = 0, accum = 0, out_dtype = 0, K = 0;
     int64_t T = 0, ld = 0, ld2 = 0;
     Pointers Y, codes, scale, zero, outl, in_codes, in_scale, in_zero, in_outl;
+    // the 4-bit cache's calls
+    tpq_kv_layout kv;
+    KvBatch batch;
+    void *cache = nullptr, *k = nullptr, *v = nullptr, *cosines = nullptr, *sines = nullptr, *workspace = nullptr;
+    int64_t ldK = 0, ldV = 0;
+    size_t ws_bytes = 0;
+    int rot = 0, rot_rows = 0, q_heads = 0, window = 0, sinks = 0;
+    float softmax_scale = 0.0f, softcap = 0.0f;
 
     bool message(const Sequence &m, Py_ssize_t count, bool meta)
     {
@@ -289,11 +355,95 @@ struct Call {
         return !(accum == -1 && PyErr_Occurred());
     }
 
+    // (L, cache, batch): what the cache's calls begin with
+    bool take_cache(PyObject *const *a, int &dev)
+    {
+        if (!kv_struct(a[0], "KvLayout", kv)) return false;
+        const Ref c(PyObject_GetAttr(a[2], s_c));
+        if (!c.p || !kv_struct(c.p, "KvBatch", batch) || !current_device(dev)) return false;
+        const at::Tensor *t = tensor_here(a[1], dev, cache);
+        if (!t) return false;
+        if (!t->is_contiguous() || batch.device != dev || kv.page_bytes < 1 || kv.D < 1)
+            return failed_check("the cache is a contiguous tensor, the batch's tensors are on the current device");
+        batch.b.n_pages = static_cast<int64_t>(t->numel()) * static_cast<int64_t>(t->element_size()) / kv.page_bytes;
+        if (batch.b.max_len == 0) {
+            const int64_t all = static_cast<int64_t>(batch.b.ld_table) * kv.page;
+            batch.b.max_len = static_cast<int32_t>(all < 0x7FFFFFFF ? all : 0x7FFFFFFF);
+        }
+        return true;
+    }
+    bool take_kv(PyObject *const *a)
+    {
+        int dev;
+        if (!take_cache(a, dev)) return false;
+        const int64_t D = kv.D;
+        int64_t heads = kv.heads, rows = -1, qh = 0;
+        switch (kind) {
+        case kKvAppend: {  // L, cache, batch, K, V, cos, sin, pairs, Q, Q_out
+            if (!head_rows(a[3], dev, "K is a bf16 [rows, heads, D]", D, heads, rows, at::kBFloat16, k, ldK) ||
+                !head_rows(a[4], dev, "V is a bf16 [rows, heads, D]", D, heads, rows, at::kBFloat16, v, ldV))
+                return false;
+            if ((a[5] == Py_None) != (a[6] == Py_None)) return failed_check("cos and sin go together");
+            if (a[5] != Py_None) {
+                const at::Tensor *c = tensor_here(a[5], dev, cosines), *n = c ? tensor_here(a[6], dev, sines) : nullptr;
+                if (!n) return false;
+                if (c->scalar_type() != at::kFloat || n->scalar_type() != at::kFloat || c->dim() != 2 || c->sizes() != n->sizes() ||
+                    !c->is_contiguous() || !n->is_contiguous() || c->size(0) > 0x7FFFFFFF || c->size(1) > D)
+                    return failed_check("cos and sin are contiguous fp32 tables [positions, rotated features / 2]");
+                rot = static_cast<int>(2 * c->size(1));
+                rot_rows = static_cast<int>(c->size(0));
+            }
+            const int turn = PyObject_IsTrue(a[7]);
+            if (turn < 0) return false;
+            accum = turn ? TPQ_ROT_PAIRS : TPQ_ROT_HALVES;
+            if (a[8] == Py_None && a[9] != Py_None) return failed_check("Q_out goes with Q");
+            if (a[8] != Py_None) {
+                if (!head_rows(a[8], dev, "Q is a bf16 [rows, q_heads, D]", D, qh, rows, at::kBFloat16, x, ld)) return false;
+                if (!head_rows(a[9] == Py_None ? a[8] : a[9], dev, "Q_out is a bf16 [rows, q_heads, D]", D, qh, rows, at::kBFloat16, out, ld2))
+                    return false;
+                q_heads = static_cast<int>(qh);
+            }
+            break;
+        }
+        case kKvRead: {  // L, cache, batch, K_out, V_out
+            if (a[3] == Py_None && a[4] == Py_None) return failed_check("K_out or V_out");
+            const at::Tensor *t = tensor(a[3] == Py_None ? a[4] : a[3]);
+            if (!t) return false;
+            const at::ScalarType type = t->scalar_type() == at::kFloat ? at::kFloat : at::kBFloat16;
+            out_dtype = type == at::kFloat ? TPQ_OUT_FP32 : TPQ_OUT_BF16;
+            if (a[3] != Py_None && !head_rows(a[3], dev, "K_out is an fp32 or bf16 [rows, heads, D]", D, heads, rows, type, k, ldK)) return false;
+            if (a[4] != Py_None && !head_rows(a[4], dev, "V_out is a [rows, heads, D] of K_out's type", D, heads, rows, type, v, ldV)) return false;
+            break;
+        }
+        default: {  // L, cache, batch, Q, out, scale, workspace, window, sinks, softcap
+            if (!head_rows(a[3], dev, "Q is a bf16 [rows, q_heads, D]", D, qh, rows, at::kBFloat16, x, ld) ||
+                !head_rows(a[4], dev, "out is a bf16 [rows, q_heads, D]", D, qh, rows, at::kBFloat16, out, ld2))
+                return false;
+            q_heads = static_cast<int>(qh);
+            const at::Tensor *t = tensor_here(a[6], dev, workspace);
+            if (!t) return false;
+            if (!t->is_contiguous()) return failed_check("the workspace is a contiguous tensor");
+            ws_bytes = static_cast<size_t>(t->numel()) * t->element_size();
+            softmax_scale = static_cast<float>(PyFloat_AsDouble(a[5]));
+            softcap = static_cast<float>(PyFloat_AsDouble(a[9]));
+            const long long w = PyLong_AsLongLong(a[7]), n = PyLong_AsLongLong(a[8]);
+            if (PyErr_Occurred()) return false;
+            if (w < 0 || w > 0x7FFFFFFF || n < 0 || n > 0x7FFFFFFF) return failed_check("window and sinks are numbers of tokens");
+            window = static_cast<int>(w);
+            sinks = static_cast<int>(n);
+            break;
+        }
+        }
+        batch.b.rows = rows;
+        return true;
+    }
+
     // args: as the Python functions take them, without the stream
     bool take(Kind k, PyObject *const *a)
     {
         kind = k;
         for (Py_ssize_t i = 0; i < kArgs[k]; ++i) arg[i].object(a[i]);
+        if (kind >= kKvAppend) return take_kv(a);
         if (!L.take(a[0])) return false;
         const int64_t E = L.p->E;
         switch (kind) {
@@ -370,6 +520,7 @@ struct Call {
             n = static_cast<int>(y.n);
             return partial_sums(y, E, Y, T, ld) && table(a[3], y.n, tab) && message(m, y.n, false);
         }
+        default: break;
         }
         return false;
     }
@@ -402,6 +553,15 @@ struct Call {
             return tpq_encode_static(L.p, plan, CU16(Y), ld, n, T, tab, U8(codes), U16(outl), s);
         case kDecodeStatic:
             return tpq_decode_reduce_static(L.p, plan, n, T, CU8(codes), CU16(outl), tab, accum, out_dtype, out, ld, s);
+        case kKvAppend:
+            return tpq_kv_append(&kv, cache, &batch.b, static_cast<const uint16_t *>(k), ldK, static_cast<const uint16_t *>(v), ldV,
+                                 static_cast<const float *>(cosines), static_cast<const float *>(sines), rot, rot_rows, accum,
+                                 static_cast<const uint16_t *>(x), ld, q_heads, static_cast<uint16_t *>(out), ld2, s);
+        case kKvRead:
+            return tpq_kv_read(&kv, cache, &batch.b, out_dtype, k, ldK, v, ldV, s);
+        case kKvAttend:
+            return tpq_kv_attention(&kv, cache, &batch.b, static_cast<const uint16_t *>(x), ld, q_heads, softmax_scale, window, sinks,
+                                    softcap, static_cast<uint16_t *>(out), ld2, workspace, ws_bytes, s);
         }
         return TPQ_ERR_UNSUPPORTED;
 #undef U8
@@ -413,7 +573,8 @@ struct Call {
     bool run(PyObject *stream) const
     {
         static const char *const names[] = {"tpq_encode", "tpq_hop", "tpq_gemm_encode", "tpq_decode_reduce",
-                                            "tpq_decode_reduce_fused", "tpq_encode_static", "tpq_decode_reduce_static"};
+                                            "tpq_decode_reduce_fused", "tpq_encode_static", "tpq_decode_reduce_static",
+                                            "tpq_kv_append", "tpq_kv_read", "tpq_kv_attention"};
         void *s;
         if (!stream_of(stream, s)) return false;
         const int rc = [&] {
@@ -624,6 +785,9 @@ PyMethodDef methods[] = {
     FAST("decode_reduce_fused", do_now<kFused>), FAST("decode_reduce_fused_call", do_make<kFused>),
     FAST("encode_static", do_now<kEncodeStatic>), FAST("encode_static_call", do_make<kEncodeStatic>),
     FAST("decode_reduce_static", do_now<kDecodeStatic>), FAST("decode_reduce_static_call", do_make<kDecodeStatic>),
+    FAST("kv_append", do_now<kKvAppend>), FAST("kv_append_call", do_make<kKvAppend>),
+    FAST("kv_read", do_now<kKvRead>), FAST("kv_read_call", do_make<kKvRead>),
+    FAST("kv_attention", do_now<kKvAttend>), FAST("kv_attention_call", do_make<kKvAttend>),
     FAST("calibrate", do_calibrate<false>), FAST("calibrate_fixed", do_calibrate<true>), FAST("plan_build", do_plan_build),
     {nullptr, nullptr, 0, nullptr},
 };
@@ -640,7 +804,8 @@ PyMODINIT_FUNC PyInit__binding(void)
     s_cuda_stream = PyUnicode_InternFromString("cuda_stream");
     s_stream = PyUnicode_InternFromString("stream");
     s_data_ptr = PyUnicode_InternFromString("data_ptr");
+    s_c = PyUnicode_InternFromString("_c");
     g_call_type = reinterpret_cast<PyTypeObject *>(PyType_FromSpec(&call_spec));
-    if (!g_call_type || !s_codes || !s_scale || !s_zero || !s_outl || !s_cuda_stream || !s_stream || !s_data_ptr) return nullptr;
+    if (!g_call_type || !s_codes || !s_scale || !s_zero || !s_outl || !s_cuda_stream || !s_stream || !s_data_ptr || !s_c) return nullptr;
     return PyModule_Create(&module);
 }

@@ -1,0 +1,78 @@
+// Declarations shared by the kernels of the 4-bit cache of keys and values (host + device).
+#pragma once
+
+#include "tpq_internal.h"
+
+namespace tpq {
+
+// The cache and the batch, as every kernel takes them.
+struct KvArgs {
+    uint8_t *cache;
+    const int32_t *table, *lens, *starts;
+    int64_t rows, n_pages, page_bytes;
+    int32_t n_seqs, ld_table, max_new;
+    int32_t heads, lg_page, ng, lg_group;  // lg_page, lg_group: logarithms of page and G
+    uint32_t cell_bytes;
+};
+
+struct KvAppendArgs {
+    const uint8_t *K, *V, *Q;
+    uint8_t *Q_out;
+    int64_t ldK, ldV, ldQ, ldQo;  // bytes
+    const float *cosines, *sines;
+    int32_t rot, rot_rows, pairs;
+    int32_t units;  // head rows of a token: 2 heads + q_heads
+};
+
+struct KvReadArgs {
+    uint8_t *K, *V;
+    int64_t ldK, ldV;  // bytes
+    int32_t fp32;
+    int32_t first, units;  // head rows of a token: [first, first + units) of the keys' and the values' heads
+};
+
+struct KvAttendArgs {
+    const uint8_t *Q;
+    uint8_t *out;
+    int64_t ldQ, ldOut;  // bytes
+    float *part;         // partial results: accumulators, then their maxima and sums
+    float *part_ml;
+    int32_t R;           // query heads per key/value head
+    int32_t window, sinks;
+    float scale, softcap;
+    int32_t splits, row_tiles;
+};
+
+// A sequence's new rows and its length; false: its starts are no range of rows.
+__device__ __forceinline__ bool kv_sequence(const KvArgs &a, int b, int64_t &row0, int &n, int &len)
+{
+    len = min(max(a.lens[b], 0), 1 << 30);
+    row0 = b;
+    n = 1;
+    if (!a.starts) return true;
+    const int s0 = a.starts[b], s1 = a.starts[b + 1];
+    row0 = s0;
+    n = s1 - s0;
+    return s0 >= 0 && s1 >= s0 && s1 <= a.rows;
+}
+
+// The cell of a position's token in head 0, and its slot there; null: absent.
+__device__ __forceinline__ uint8_t *kv_cell(const KvArgs &a, int b, int pos, int &slot)
+{
+    slot = pos & ((1 << a.lg_page) - 1);
+    if (pos < 0 || pos >> a.lg_page >= a.ld_table) return nullptr;
+    const int id = a.table[static_cast<int64_t>(b) * a.ld_table + (pos >> a.lg_page)];
+    if (static_cast<uint32_t>(id) >= static_cast<uint64_t>(a.n_pages)) return nullptr;
+    return a.cache + id * a.page_bytes;
+}
+
+// ---- host side ------------------------------------------------------------------------------
+int kv_check_layout(const tpq_kv_layout *L);
+int kv_check_batch(const tpq_kv_layout *L, const tpq_kv_batch *batch);
+KvArgs kv_args(const tpq_kv_layout *L, const void *cache, const tpq_kv_batch *batch);
+int launch_kv_append(const KvArgs &a, const KvAppendArgs &p, int D, hipStream_t s);
+int launch_kv_read(const KvArgs &a, const KvReadArgs &p, int D, hipStream_t s);
+size_t kv_attend_workspace_bytes(const KvArgs &a, int D, int R, int max_len);
+int launch_kv_attend(const KvArgs &a, KvAttendArgs p, int D, int max_len, void *workspace, hipStream_t s);
+
+}  // namespace tpq
