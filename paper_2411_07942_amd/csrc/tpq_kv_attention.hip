@@ -2,6 +2,8 @@
 //
 //   s_j = scale * q . k_j,  out = sum_j exp(s_j) v_j / sum_j exp(s_j),  k_j, v_j = code * scale_j + zero_j per group
 #include <algorithm>
+#include <type_traits>
+#include <utility>
 
 #include "tpq_device.h"
 #include "tpq_kv.h"
@@ -38,19 +40,50 @@ constexpr int kKvMinTiles = 4;
 __device__ __forceinline__ int kv_share(int tiles, int splits) { return max((tiles + splits - 1) / splits, kKvMinTiles); }
 __device__ __forceinline__ int kv_live(int tiles, int share) { return max((tiles + share - 1) / share, 1); }
 
-__device__ __forceinline__ float group4_max(float v)  // over lanes l, l ^ 16, l ^ 32, l ^ 48
+// Over lanes l, l ^ 16, l ^ 32, l ^ 48, in all of them (the swaps leave the rows of 16 and the halves beside each other).
+__device__ __forceinline__ float group4_max(float v)
 {
-    v = fmaxf(v, __shfl_xor(v, 16, 64));
-    return fmaxf(v, __shfl_xor(v, 32, 64));
+    const uint32_t x = __float_as_uint(v);
+    const auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+    v = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    const uint32_t y = __float_as_uint(v);
+    const auto t = __builtin_amdgcn_permlane32_swap(y, y, false, false);
+    return fmaxf(__uint_as_float(t[0]), __uint_as_float(t[1]));
 }
 __device__ __forceinline__ float group4_sum(float v)
 {
-    v += __shfl_xor(v, 16, 64);
-    return v + __shfl_xor(v, 32, 64);
+    const uint32_t x = __float_as_uint(v);
+    const auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+    v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    const uint32_t y = __float_as_uint(v);
+    const auto t = __builtin_amdgcn_permlane32_swap(y, y, false, false);
+    return __uint_as_float(t[0]) + __uint_as_float(t[1]);
+}
+
+// The value that lane N of the caller's row of 16 holds.
+template <int N>
+__device__ __forceinline__ float of_row(float v)
+{
+    return dpp_f32<0x150 + N>(v);
+}
+template <int N, typename F, int... I>
+__device__ __forceinline__ void for_each_of(F &&f, std::integer_sequence<int, I...>)
+{
+    (f(std::integral_constant<int, I>{}), ...);
+}
+template <int N, typename F>
+__device__ __forceinline__ void for_each(F &&f)
+{
+    for_each_of<N>(f, std::make_integer_sequence<int, N>{});
 }
 
 // codes of a dword -> 128 + code in bf16 (8 bits of significand: exact), nibbles t and 4 + t a pair
-__device__ __forceinline__ uint32_t code_pair(uint32_t w) { return (w & 0x000F000Fu) | 0x43004300u; }
+// (one instruction with both constants in registers, one of them scalar: neither may be a literal)
+struct CodePair {
+    uint32_t mask = 0x000F000Fu, base = 0x43004300u;
+    __device__ __forceinline__ CodePair() { asm volatile("" : "+s"(mask), "+v"(base)); }
+    __device__ __forceinline__ uint32_t operator()(uint32_t w) const { return (w & mask) | base; }
+};
 
 // What a wave reads of a step's 32 tokens: lane (m, g) = (l % 16, l / 16).
 template <int D, int NG>
@@ -58,17 +91,18 @@ struct KvRaw {
     static constexpr int KW = D / 32, VW = D == 256 ? 2 : 1;  // words: of a token's quarter of K codes; of a token's chunk of V codes
     uint32_t k[2][KW];       // tokens 16 j + m
     uint32_t v[2][4][VW];    // tokens 16 j + 4 g + i
-    u32x4 km[2][NG], vm[2][NG];
+    uint32_t meta[NG];       // lane 8 kv + 4 j + i of a row of 16: keys' (kv = 0) or values' scale and zero of token 16 j + 4 g + i
     bool bad[2];             // (uniform) a page that is none
 };
 
 template <int D, int NG, int NR>
-__global__ __launch_bounds__(256) void k_kv_attend_few(KvArgs a, KvAttendArgs p)
+__global__ __launch_bounds__(256, D * NR <= 128 && NG <= 2 ? 3 : 2) void k_kv_attend_few(KvArgs a, KvAttendArgs p)
 {
     constexpr int KK = D / 32, NT = D / 16, KPG = KK / NG, TPG = NT / NG, ROWS = 16 * NR;
     typedef KvRaw<D, NG> Raw;
     __shared__ float sO[2][ROWS][D + 4];
     __shared__ float sM[2][ROWS], sL[2][ROWS];
+    const CodePair code_pair;
     const uint32_t ln = threadIdx.x & 63u, m = ln & 15u, g = ln >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int split = blockIdx.x % p.splits, rt = blockIdx.x / p.splits, h = blockIdx.y, b = blockIdx.z;
@@ -99,7 +133,8 @@ __global__ __launch_bounds__(256) void k_kv_attend_few(KvArgs a, KvAttendArgs p)
             float sum = 0.0f;
 #pragma unroll
             for (int kk = gr * KPG; kk < (gr + 1) * KPG; ++kk) {
-                const u32x4 w = *reinterpret_cast<const u32x4 *>(src + 64 * kk);
+                u32x4 w = *reinterpret_cast<const u32x4 *>(src + 64 * kk);
+                if (p.scale < 0.0f) w ^= 0x80008000u;  // (scores are then multiplied by |scale|: their order is the products')
                 q[r][kk] = __builtin_bit_cast(bf16x8_t, w);
                 const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
@@ -112,32 +147,40 @@ __global__ __launch_bounds__(256) void k_kv_attend_few(KvArgs a, KvAttendArgs p)
     const int n_blocks = (min(len, a.ld_table << a.lg_page) + 15) / 16;  // blocks of 16 tokens that exist
     const uint32_t page_len = 1u << a.lg_page, page_mask = page_len - 1u;
     const int32_t *table = a.table + static_cast<int64_t>(b) * a.ld_table;
-    auto load = [&](Raw &raw, int tile) {
+    // The page numbers of the wave's next 32 steps, two a step, one a lane: one load's latency for all of them.
+    auto pages_of = [&](int v) {
+        const int tile = span.tile(min(v + 4 * static_cast<int>(ln >> 1), v1 - 1));
+        const int block = min(2 * tile + static_cast<int>(ln & 1u), n_blocks - 1);
+        return table[(16 * block) >> a.lg_page];
+    };
+    auto load = [&](Raw &raw, int v, int pages, int nth) {
+        const int tile = span.tile(v);
+        const uint8_t *metas[2];
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
             const int block = min(2 * tile + j, n_blocks - 1);
             const uint32_t slot = (16u * block) & page_mask;
-            const int id = table[(16 * block) >> a.lg_page];
+            const int id = __builtin_amdgcn_readlane(pages, 2 * nth + j);
             raw.bad[j] = static_cast<uint32_t>(id) >= static_cast<uint64_t>(a.n_pages);
             const uint8_t *cell = a.cache + (raw.bad[j] ? 0 : id) * a.page_bytes + static_cast<int64_t>(h) * a.cell_bytes;
-            const uint8_t *k = cell + (slot + m) * (D / 2) + g * (D / 8);
+            const uint8_t *k = cell + slot * (D / 2);
+            const uint32_t ko = m * (D / 2) + g * (D / 8);
 #pragma unroll
-            for (int w = 0; w < Raw::KW; ++w) raw.k[j][w] = reinterpret_cast<const uint32_t *>(k)[w];
-            const uint8_t *v = cell + page_len * (D / 2) + (slot + 4 * g) * (D / 2) + (D == 64 ? m / 2 * 4 : m * (D / 32));
+            for (int w = 0; w < Raw::KW; ++w) raw.k[j][w] = reinterpret_cast<const uint32_t *>(k + ko)[w];
+            const uint8_t *vc = cell + (page_len + slot) * (D / 2);
+            const uint32_t vo = g * (2 * D) + (D == 64 ? m / 2 * 4 : m * (D / 32));
 #pragma unroll
             for (int i = 0; i < 4; ++i)
 #pragma unroll
-                for (int w = 0; w < Raw::VW; ++w) raw.v[j][i][w] = reinterpret_cast<const uint32_t *>(v + i * (D / 2))[w];
-            const uint8_t *meta = cell + page_len * D + 4 * (slot + 4 * g);
-#pragma unroll
-            for (int gr = 0; gr < NG; ++gr) {
-                raw.km[j][gr] = *reinterpret_cast<const u32x4 *>(meta + 4 * (gr * page_len));
-                raw.vm[j][gr] = *reinterpret_cast<const u32x4 *>(meta + 4 * ((NG + gr) * page_len));
-            }
+                for (int w = 0; w < Raw::VW; ++w) raw.v[j][i][w] = reinterpret_cast<const uint32_t *>(vc + vo + i * (D / 2))[w];
+            metas[j] = cell + page_len * D + 4 * slot;
         }
+        const uint8_t *meta = (m & 4u ? metas[1] : metas[0]) + (m & 8u ? 4 * NG * page_len : 0u) + 16 * g + 4 * (m & 3u);
+#pragma unroll
+        for (int gr = 0; gr < NG; ++gr) raw.meta[gr] = *reinterpret_cast<const uint32_t *>(meta + 4 * (gr * page_len));
     };
 
-    f32x4 o[NR][NT], oc[NR][NG];
+    f32x4 o[NR][NT], oc[NR];  // accumulators; row gr of oc: 128 * (sum of group gr's weights as the products see them)
     float zs[NR][NG], mx[NR], l[NR];
 #pragma unroll
     for (int r = 0; r < NR; ++r) {
@@ -145,128 +188,183 @@ __global__ __launch_bounds__(256) void k_kv_attend_few(KvArgs a, KvAttendArgs p)
         l[r] = 0.0f;
 #pragma unroll
         for (int t = 0; t < NT; ++t) o[r][t] = f32x4{0, 0, 0, 0};
+        oc[r] = f32x4{0, 0, 0, 0};
 #pragma unroll
-        for (int gr = 0; gr < NG; ++gr) {
-            oc[r][gr] = f32x4{0, 0, 0, 0};
-            zs[r][gr] = 0.0f;
-        }
+        for (int gr = 0; gr < NG; ++gr) zs[r][gr] = 0.0f;
     }
     const float log2e = 1.44269504f;
-    const u32x4 c128 = {0x43004300u, 0x43004300u, 0x43004300u, 0x43004300u};
 
-    for (int v = split * share + wave; v < v1; v += 4) {
-        Raw raw;
-        const int tile = span.tile(v), t0 = tile * kKvTile;
-        load(raw, tile);
+    // scores in powers of two: exp(s) = 2^(s log2 e)
+    const float k_score = p.softcap > 0.0f ? 1.0f : fabsf(p.scale) * log2e;
+    const float cap_in = p.softcap > 0.0f ? fabsf(p.scale) / p.softcap * 2.0f * log2e : 0.0f, cap_out = p.softcap * log2e;
+
+    auto step = [&](const Raw &raw, int v) {
+        const int t0 = span.tile(v) * kKvTile;
         const bool whole = t0 + kKvTile - 1 <= lo && (p.window == 0 || t0 > hi - p.window || t0 + kKvTile <= p.sinks) && !raw.bad[0] && !raw.bad[1];
+        float s[NR][2][4];
+        bool vis[NR][2][4];
+        for_each<2>([&](auto jj) {
+            constexpr int J = decltype(jj)::value;
+#pragma unroll
+            for (int gr = 0; gr < NG; ++gr) {
+                f32x4 acc[NR];
+#pragma unroll
+                for (int r = 0; r < NR; ++r) {
+                    float c0 = -128.0f * qs[r][gr];
+                    asm volatile("" : "+v"(c0));  // (anew in every step: kept outside the loop it would take four registers)
+                    acc[r] = f32x4{c0, c0, c0, c0};
+                }
+#pragma unroll
+                for (int kk = gr * KPG; kk < (gr + 1) * KPG; ++kk) {
+                    const uint32_t w = raw.k[J][kk];
+                    const u32x4 c = {code_pair(w), code_pair(w >> 4), code_pair(w >> 8), code_pair(w >> 12)};
+#pragma unroll
+                    for (int r = 0; r < NR; ++r)
+                        acc[r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, c), q[r][kk], acc[r], 0, 0, 0);
+                }
+                const float sc = bf16_lo_to_f32(raw.meta[gr]), ze = bf16_hi_to_f32(raw.meta[gr]);
+                for_each<4>([&](auto i) {
+                    constexpr int I = decltype(i)::value;
+                    // (products, whose operand the exchange goes into; multiply-adds would take a move for each)
+#pragma unroll
+                    for (int r = 0; r < NR; ++r) {
+                        const float x = of_row<4 * J + I>(sc) * acc[r][I], z = of_row<4 * J + I>(ze) * qs[r][gr];
+                        s[r][J][I] = gr == 0 ? x + z : (s[r][J][I] + x) + z;
+                    }
+                });
+            }
+        });
 #pragma unroll
         for (int r = 0; r < NR; ++r) {
-            float s[2][4];
-            bool vis[2][4];
+            if (p.softcap > 0.0f) {
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) s[j][i] = 0.0f;
-#pragma unroll
-                for (int gr = 0; gr < NG; ++gr) {
-                    const float c0 = -128.0f * qs[r][gr];
-                    f32x4 acc = {c0, c0, c0, c0};
-#pragma unroll
-                    for (int kk = gr * KPG; kk < (gr + 1) * KPG; ++kk) {
-                        const uint32_t w = raw.k[j][kk];
-                        const u32x4 c = {code_pair(w), code_pair(w >> 4), code_pair(w >> 8), code_pair(w >> 12)};
-                        acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, c), q[r][kk], acc, 0, 0, 0);
-                    }
-                    const uint32_t meta[4] = {raw.km[j][gr].x, raw.km[j][gr].y, raw.km[j][gr].z, raw.km[j][gr].w};
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        s[j][i] = __builtin_fmaf(bf16_lo_to_f32(meta[i]), acc[i], __builtin_fmaf(bf16_hi_to_f32(meta[i]), qs[r][gr], s[j][i]));
-                }
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    if (p.softcap > 0.0f) {
-                        // cap * tanh(x / cap) = cap - 2 cap / (exp(2 x / cap) + 1)
-                        const float e = __builtin_amdgcn_exp2f(s[j][i] * (p.scale / p.softcap * 2.0f * log2e));
-                        s[j][i] = (p.softcap - 2.0f * p.softcap / (e + 1.0f)) * log2e;
-                    } else {
-                        s[j][i] *= p.scale * log2e;
-                    }
-                    vis[j][i] = true;
-                    if (!whole) {
-                        const int key = t0 + 16 * j + 4 * static_cast<int>(g) + i;
-                        vis[j][i] = key <= pos[r] && (p.window == 0 || key > pos[r] - p.window || key < p.sinks) && !raw.bad[j] &&
-                                    key < 16 * n_blocks;
-                        s[j][i] = vis[j][i] ? s[j][i] : kKvLowest;
-                    }
+                for (int x = 0; x < 8; ++x) {
+                    // cap tanh(x / cap) = cap - 2 cap / (exp(2 x / cap) + 1)
+                    const float e = __builtin_amdgcn_exp2f(s[r][x >> 2][x & 3] * cap_in) + 1.0f;
+                    s[r][x >> 2][x & 3] = __builtin_fmaf(-2.0f * cap_out, __builtin_amdgcn_rcpf(e), cap_out);
                 }
             }
-            float top = s[0][0];
+            if (!whole) {
 #pragma unroll
-            for (int j = 0; j < 2; ++j)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) top = fmaxf(top, s[j][i]);
-            const float now = fmaxf(mx[r], group4_max(top)), alpha = __builtin_amdgcn_exp2f(mx[r] - now);
-            mx[r] = now;
-            l[r] *= alpha;
-#pragma unroll
-            for (int t = 0; t < NT; ++t) o[r][t] *= alpha;
-#pragma unroll
-            for (int gr = 0; gr < NG; ++gr) {
-                oc[r][gr] *= alpha;
-                zs[r][gr] *= alpha;
-            }
-            float e[2][4];
-#pragma unroll
-            for (int j = 0; j < 2; ++j)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    e[j][i] = __builtin_amdgcn_exp2f(s[j][i] - now);
-                    e[j][i] = vis[j][i] ? e[j][i] : 0.0f;
-                    l[r] += e[j][i];
+                for (int x = 0; x < 8; ++x) {
+                    const int j = x >> 2, i = x & 3, key = t0 + 16 * j + 4 * static_cast<int>(g) + i;
+                    vis[r][j][i] = key <= pos[r] && (p.window == 0 || key > pos[r] - p.window || key < p.sinks) && !raw.bad[j] && key < 16 * n_blocks;
+                    s[r][j][i] = vis[r][j][i] ? s[r][j][i] : kKvLowest;
                 }
+            }
+            float top = s[r][0][0];
 #pragma unroll
-            for (int gr = 0; gr < NG; ++gr) {
+            for (int x = 1; x < 8; ++x) top = fmaxf(top, s[r][x >> 2][x & 3]);
+            top *= k_score;
+            // The maximum only follows where a weight would pass 2^8: weights are relative anyway, and a step without it saves
+            // the accumulators' rescaling.
+            if (__builtin_amdgcn_ballot_w64(top > mx[r] + 8.0f)) {
+                const float now = fmaxf(mx[r], group4_max(top)), alpha = __builtin_amdgcn_exp2f(mx[r] - now);
+                mx[r] = now;
+                l[r] *= alpha;
+#pragma unroll
+                for (int t = 0; t < NT; ++t) o[r][t] *= alpha;
+                oc[r] *= alpha;
+#pragma unroll
+                for (int gr = 0; gr < NG; ++gr) zs[r][gr] *= alpha;
+            }
+#pragma unroll
+            for (int x = 0; x < 8; ++x) {
+                float &e = s[r][x >> 2][x & 3];  // the weight, in the score's place
+                e = __builtin_amdgcn_exp2f(__builtin_fmaf(e, k_score, -mx[r]));
+                if (!whole) e = vis[r][x >> 2][x & 3] ? e : 0.0f;
+                l[r] += e;
+            }
+        }
+#pragma unroll
+        for (int gr = 0; gr < NG; ++gr) {
+            bf16x8_t bh[NR], bl[NR];
+            const float sc = bf16_lo_to_f32(raw.meta[gr]), ze = bf16_hi_to_f32(raw.meta[gr]);
+#pragma unroll
+            for (int r = 0; r < NR; ++r) {
                 u32x4 ph, pl;
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    const uint32_t meta[4] = {raw.vm[j][gr].x, raw.vm[j][gr].y, raw.vm[j][gr].z, raw.vm[j][gr].w};
+                for_each<2>([&](auto jj) {
+                    constexpr int J = decltype(jj)::value;
                     float w[4];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const uint32_t mt = vis[j][i] ? meta[i] : 0u;  // (what lies behind a hidden key may be anything)
-                        w[i] = e[j][i] * bf16_lo_to_f32(mt);
-                        zs[r][gr] = __builtin_fmaf(e[j][i], bf16_hi_to_f32(mt), zs[r][gr]);
+                    for_each<4>([&](auto i) {
+                        constexpr int I = decltype(i)::value;
+                        w[I] = of_row<8 + 4 * J + I>(sc) * s[r][J][I];
+                    });
+                    if (whole) {
+                        for_each<4>([&](auto i) {
+                            constexpr int I = decltype(i)::value;
+                            zs[r][gr] += of_row<8 + 4 * J + I>(ze) * s[r][J][I];
+                        });
+                    } else {  // (what lies behind a hidden key may be anything)
+                        for_each<4>([&](auto i) {
+                            constexpr int I = decltype(i)::value;
+                            const float z = of_row<8 + 4 * J + I>(ze) * s[r][J][I];
+                            zs[r][gr] += vis[r][J][I] ? z : 0.0f;
+                            w[I] = vis[r][J][I] ? w[I] : 0.0f;
+                        });
                     }
 #pragma unroll
                     for (int i = 0; i < 4; i += 2) {
                         const uint32_t hi2 = pack_bf16x2(w[i], w[i + 1]);
-                        ph[2 * j + i / 2] = hi2;
-                        pl[2 * j + i / 2] = pack_bf16x2(w[i] - bf16_lo_to_f32(hi2), w[i + 1] - bf16_hi_to_f32(hi2));
+                        ph[2 * J + i / 2] = hi2;
+                        pl[2 * J + i / 2] = pack_bf16x2(w[i] - bf16_lo_to_f32(hi2), w[i + 1] - bf16_hi_to_f32(hi2));
                     }
+                });
+                bh[r] = __builtin_bit_cast(bf16x8_t, ph);
+                bl[r] = __builtin_bit_cast(bf16x8_t, pl);
+            }
+            uint32_t one = NG == 1 || m == static_cast<uint32_t>(gr) ? code_pair.base : 0u;
+            if (NG > 1) asm volatile("" : "+v"(one));
+            const bf16x8_t ones = __builtin_bit_cast(bf16x8_t, (u32x4{one, one, one, one}));
+#pragma unroll
+            for (int r = 0; r < NR; ++r) {
+                oc[r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, bh[r], oc[r], 0, 0, 0);
+                oc[r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, bl[r], oc[r], 0, 0, 0);
+            }
+#pragma unroll
+            for (int t = gr * TPG; t < (gr + 1) * TPG; ++t) {
+                const int word = t / 8, byte = (t % 8) / 2;
+                const uint32_t at = D == 64 ? byte + 2 * (m & 1u) : byte;
+                const uint32_t sel = 0x0C000C00u | ((4u + at) << 16) | at;
+                u32x4 c;
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                    const int j = x >> 1, i = 2 * (x & 1);
+                    const uint32_t y = __builtin_amdgcn_perm(raw.v[j][i + 1][word], raw.v[j][i][word], sel);
+                    c[x] = code_pair(t & 1 ? y >> 4 : y);
                 }
-                const bf16x8_t bh = __builtin_bit_cast(bf16x8_t, ph), bl = __builtin_bit_cast(bf16x8_t, pl);
-                const bf16x8_t ac = __builtin_bit_cast(bf16x8_t, c128);
-                oc[r][gr] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ac, bh, oc[r][gr], 0, 0, 0);
-                oc[r][gr] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ac, bl, oc[r][gr], 0, 0, 0);
+                const bf16x8_t av = __builtin_bit_cast(bf16x8_t, c);
 #pragma unroll
-                for (int t = gr * TPG; t < (gr + 1) * TPG; ++t) {
-                    const int word = t / 8, byte = (t % 8) / 2;
-                    const uint32_t at = D == 64 ? byte + 2 * (m & 1u) : byte;
-                    const uint32_t sel = 0x0C000C00u | ((4u + at) << 16) | at;
-                    u32x4 c;
-#pragma unroll
-                    for (int j = 0; j < 2; ++j)
-#pragma unroll
-                        for (int i = 0; i < 4; i += 2) {
-                            const uint32_t x = __builtin_amdgcn_perm(raw.v[j][i + 1][word], raw.v[j][i][word], sel);
-                            c[2 * j + i / 2] = code_pair(t & 1 ? x >> 4 : x);
-                        }
-                    const bf16x8_t av = __builtin_bit_cast(bf16x8_t, c);
-                    o[r][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av, bh, o[r][t], 0, 0, 0);
-                    o[r][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av, bl, o[r][t], 0, 0, 0);
+                for (int r = 0; r < NR; ++r) {
+                    o[r][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av, bh[r], o[r][t], 0, 0, 0);
+                    o[r][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av, bl[r], o[r][t], 0, 0, 0);
                 }
             }
+            if (NG > 1) __builtin_amdgcn_sched_barrier(0);  // (one group's codes and weights in registers at a time)
         }
+    };
+
+    // A step's loads are issued before the step in front of it is worked on.
+    const int v0 = split * share + wave;
+    Raw even, odd;
+    int pages = 0;
+    if (v0 < v1) {
+        pages = pages_of(v0);
+        load(even, v0, pages, 0);
+    }
+    for (int v = v0, nth = 0; v < v1; v += 8) {
+        if (v + 4 < v1) load(odd, v + 4, pages, nth + 1);
+        __builtin_amdgcn_sched_barrier(0);
+        step(even, v);
+        if (v + 4 >= v1) break;
+        nth += 2;
+        if (nth == 32) {
+            nth = 0;
+            pages = pages_of(v + 8);
+        }
+        if (v + 8 < v1) load(even, v + 8, pages, nth);
+        __builtin_amdgcn_sched_barrier(0);
+        step(odd, v + 4);
     }
 
     // 128 * (sum of the weights) off the codes, the zeros' share on
@@ -275,9 +373,9 @@ __global__ __launch_bounds__(256) void k_kv_attend_few(KvArgs a, KvAttendArgs p)
         l[r] = group4_sum(l[r]);
 #pragma unroll
         for (int gr = 0; gr < NG; ++gr) {
-            const float z = group4_sum(zs[r][gr]);
+            const float z = group4_sum(zs[r][gr]), c = NG == 1 ? oc[r][0] : __shfl(oc[r][gr & 3], 16 * (gr >> 2) + m, 64);
 #pragma unroll
-            for (int t = gr * TPG; t < (gr + 1) * TPG; ++t) o[r][t] = o[r][t] - oc[r][gr] + z;
+            for (int t = gr * TPG; t < (gr + 1) * TPG; ++t) o[r][t] = o[r][t] - c + z;
         }
     }
     // the four waves' results into wave 0's: 2 and 3 to 0 and 1, then 1 to 0
@@ -371,10 +469,10 @@ struct KvChoice {
     int rows, row_tiles, splits;
 };
 
-static KvChoice choose(const KvArgs &a, int R, int max_len, int compute_units)
+static KvChoice choose(const KvArgs &a, int D, int R, int max_len, int compute_units)
 {
     KvChoice c;
-    c.rows = 16;
+    c.rows = D <= 128 && a.ng == 1 && a.max_new * R > 16 ? 32 : 16;
     c.row_tiles = (a.max_new * R + c.rows - 1) / c.rows;
     const int64_t tiles = (max_len + kKvTile - 1) / kKvTile + 1, groups = static_cast<int64_t>(a.n_seqs) * a.heads * c.row_tiles;
     const int64_t want = (4ll * compute_units + groups - 1) / groups;
@@ -386,7 +484,7 @@ size_t kv_attend_workspace_bytes(const KvArgs &a, int D, int R, int max_len)
 {
     int cu;
     if (compute_units_of_current_device(&cu) != hipSuccess) return 0;
-    const KvChoice c = choose(a, R, max_len, cu);
+    const KvChoice c = choose(a, D, R, max_len, cu);
     if (c.splits == 1) return 16;
     return static_cast<size_t>(a.n_seqs) * a.heads * c.row_tiles * c.splits * c.rows * (D + 2) * sizeof(float);
 }
@@ -407,12 +505,14 @@ int launch_kv_attend(const KvArgs &a, KvAttendArgs p, int D, int max_len, void *
     int cu;
     const hipError_t e = compute_units_of_current_device(&cu);
     if (e != hipSuccess) return hip_result(e);
-    const KvChoice c = choose(a, p.R, max_len, cu);
+    const KvChoice c = choose(a, D, p.R, max_len, cu);
     p.splits = c.splits;
     p.row_tiles = c.row_tiles;
     p.part = static_cast<float *>(workspace);
     p.part_ml = p.part + static_cast<size_t>(a.n_seqs) * a.heads * c.row_tiles * c.splits * c.rows * D;
-    const auto kernel = D == 64 ? few_kernel<64>(a.ng) : D == 128 ? few_kernel<128>(a.ng) : few_kernel<256>(a.ng);
+    const auto kernel = D == 256 ? few_kernel<256>(a.ng)
+                        : c.rows == 32 ? (D == 64 ? k_kv_attend_few<64, 1, 2> : k_kv_attend_few<128, 1, 2>)
+                                       : (D == 64 ? few_kernel<64>(a.ng) : few_kernel<128>(a.ng));
     launch_kernel(kernel, dim3(static_cast<uint32_t>(c.splits) * c.row_tiles, a.heads, a.n_seqs), dim3(256), 0, s, a, p);
     if (c.splits > 1) {
         const int per = 256 / (D / 4);
