@@ -2,6 +2,7 @@
 //
 //   s_j = scale * q . k_j,  out = sum_j exp(s_j) v_j / sum_j exp(s_j),  k_j, v_j = code * scale_j + zero_j per group
 #include <algorithm>
+#include <atomic>
 #include <type_traits>
 #include <utility>
 
@@ -13,7 +14,7 @@ namespace tpq {
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
-constexpr int kKvTile = 32;            // tokens of a step of a wave
+constexpr int kKvTile = 32;            // tokens of a step of a wave (few rows)
 constexpr float kKvLowest = -3.0e38f;  // the running maximum before the first score
 
 // The steps that rows at positions lo .. hi go through: the tiles that hold visible first tokens, then those from the first
@@ -22,23 +23,54 @@ struct KvSpan {
     int first, start, tiles;  // tiles of first tokens, first tile of the rest, all tiles
     __device__ __forceinline__ int tile(int v) const { return v < first ? v : start + (v - first); }
 };
-__device__ __forceinline__ KvSpan kv_span(const KvArgs &a, int window, int sinks, int lo, int hi, int len)
+template <int TOK>
+__device__ __forceinline__ KvSpan kv_span(const KvArgs &a, const KvAttendArgs &p, int lo, int hi, int len)
 {
     const int end = min(min(hi + 1, len), a.ld_table << a.lg_page);
     KvSpan s = {0, 0, 0};
     if (end <= 0) return s;
-    const int last = (end + kKvTile - 1) / kKvTile;
-    if (window > 0) {
-        s.start = max(lo - window + 1, 0) / kKvTile;
-        s.first = min((min(sinks, end) + kKvTile - 1) / kKvTile, s.start);
+    const int last = (end + TOK - 1) / TOK;
+    if (p.window > 0) {
+        s.start = max(lo - p.window + 1, 0) / TOK;
+        s.first = min((min(p.sinks, end) + TOK - 1) / TOK, s.start);
     }
     s.tiles = s.first + max(last - s.start, 0);
     return s;
 }
-// Steps of one split of `splits`, and how many splits have any (at least one).
-constexpr int kKvMinTiles = 4;
-__device__ __forceinline__ int kv_share(int tiles, int splits) { return max((tiles + splits - 1) / splits, kKvMinTiles); }
-__device__ __forceinline__ int kv_live(int tiles, int share) { return max((tiles + share - 1) / share, 1); }
+
+// A workgroup's rows: a tile of `rows` of a sequence's rows of a key/value head (row i R + r: query head r of new token
+// i), and a share of the steps that they go through.  Every tile of a sequence has shares of one size, that of its last
+// tile cut into `splits`.
+struct KvShare {
+    int64_t row0;
+    int n_rows, base, len;  // rows of the sequence and head, position of row 0, tokens
+    int lo, hi;             // first and last position among the tile's rows
+    KvSpan span;
+    int live, share;        // shares that have steps (at least one), steps of a share
+};
+template <int TOK>
+__device__ __forceinline__ bool kv_share(const KvArgs &a, const KvAttendArgs &p, int b, int rt, int rows, KvShare &s)
+{
+    int n;
+    if (!kv_sequence(a, b, s.row0, n, s.len)) return false;
+    s.base = s.len - n;
+    n = min(n, a.max_new);
+    s.n_rows = n * p.R;
+    if (rt * rows >= s.n_rows) return false;
+    s.lo = s.base + p.by_R.of(rt * rows);
+    s.hi = s.base + p.by_R.of(min((rt + 1) * rows, s.n_rows) - 1);
+    s.span = kv_span<TOK>(a, p, s.lo, s.hi, s.len);
+    s.share = s.span.tiles;
+    s.live = 1;
+    if (p.splits > 1) {
+        const int last = (s.n_rows - 1) / rows * rows;
+        const int most = kv_span<TOK>(a, p, s.base + p.by_R.of(last), s.base + n - 1, s.len).tiles;
+        s.share = max(p.by_splits.of(most + p.splits - 1), p.min_tiles);
+        s.live = 1;
+        for (int at = s.share; at < s.span.tiles; at += s.share) ++s.live;
+    }
+    return true;
+}
 
 // Over lanes l, l ^ 16, l ^ 32, l ^ 48, in all of them (the swaps leave the rows of 16 and the halves beside each other).
 __device__ __forceinline__ float group4_max(float v)
@@ -105,17 +137,12 @@ __global__ __launch_bounds__(256, D * NR <= 128 && NG <= 2 ? 3 : 2) void k_kv_at
     const CodePair code_pair;
     const uint32_t ln = threadIdx.x & 63u, m = ln & 15u, g = ln >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int split = blockIdx.x % p.splits, rt = blockIdx.x / p.splits, h = blockIdx.y, b = blockIdx.z;
-    int64_t row0;
-    int n, len;
-    if (!kv_sequence(a, b, row0, n, len)) return;
-    const int n_rows = min(n, a.max_new) * p.R;
-    if (rt * ROWS >= n_rows) return;
-    const int base = len - n;  // position of row 0's token
-    const int lo = base + rt * ROWS / p.R, hi = base + (min((rt + 1) * ROWS, n_rows) - 1) / p.R;
-    const KvSpan span = kv_span(a, p.window, p.sinks, lo, hi, len);
-    const int share = kv_share(span.tiles, p.splits), live = kv_live(span.tiles, share);
-    if (split >= live) return;
+    const int rt = p.by_splits.of(blockIdx.x), split = blockIdx.x - rt * p.splits, h = blockIdx.y, b = blockIdx.z;
+    KvShare w;
+    if (!kv_share<kKvTile>(a, p, b, rt, ROWS, w) || split >= w.live) return;
+    const int64_t row0 = w.row0;
+    const int n_rows = w.n_rows, base = w.base, len = w.len, lo = w.lo, hi = w.hi, live = w.live, share = w.share;
+    const KvSpan span = w.span;
     const int v1 = min((split + 1) * share, span.tiles);
 
     // queries: column m of the products' right operand
@@ -125,7 +152,7 @@ __global__ __launch_bounds__(256, D * NR <= 128 && NG <= 2 ? 3 : 2) void k_kv_at
 #pragma unroll
     for (int r = 0; r < NR; ++r) {
         const int row = rt * ROWS + 16 * r + static_cast<int>(m);
-        const int rc = min(row, n_rows - 1), i = rc / p.R;
+        const int rc = min(row, n_rows - 1), i = p.by_R.of(rc);
         pos[r] = base + i;
         const uint8_t *src = p.Q + (row0 + i) * p.ldQ + (h * p.R + rc - i * p.R) * (2 * D) + 16 * g;
 #pragma unroll
@@ -195,6 +222,7 @@ __global__ __launch_bounds__(256, D * NR <= 128 && NG <= 2 ? 3 : 2) void k_kv_at
     const float log2e = 1.44269504f;
 
     // scores in powers of two: exp(s) = 2^(s log2 e)
+    const int window = p.window > 0 ? p.window : 1 << 30;
     const float k_score = p.softcap > 0.0f ? 1.0f : fabsf(p.scale) * log2e;
     const float cap_in = p.softcap > 0.0f ? fabsf(p.scale) / p.softcap * 2.0f * log2e : 0.0f, cap_out = p.softcap * log2e;
 
@@ -248,7 +276,7 @@ __global__ __launch_bounds__(256, D * NR <= 128 && NG <= 2 ? 3 : 2) void k_kv_at
 #pragma unroll
                 for (int x = 0; x < 8; ++x) {
                     const int j = x >> 2, i = x & 3, key = t0 + 16 * j + 4 * static_cast<int>(g) + i;
-                    vis[r][j][i] = key <= pos[r] && (p.window == 0 || key > pos[r] - p.window || key < p.sinks) && !raw.bad[j] && key < 16 * n_blocks;
+                    vis[r][j][i] = (key <= pos[r]) & ((key > pos[r] - window) | (key < p.sinks)) & !raw.bad[j] & (key < 16 * n_blocks);
                     s[r][j][i] = vis[r][j][i] ? s[r][j][i] : kKvLowest;
                 }
             }
@@ -412,7 +440,7 @@ __global__ __launch_bounds__(256, D * NR <= 128 && NG <= 2 ? 3 : 2) void k_kv_at
         const int row = rt * ROWS + 16 * r + static_cast<int>(m);
         if (row >= n_rows) continue;
         if (live == 1) {
-            const int i = row / p.R;
+            const int i = p.by_R.of(row);
             uint8_t *dst = p.out + (row0 + i) * p.ldOut + (h * p.R + row - i * p.R) * (2 * D) + 8 * g;
             const float inv = l[r] > 0.0f ? 1.0f / l[r] : 0.0f;
 #pragma unroll
@@ -428,56 +456,593 @@ __global__ __launch_bounds__(256, D * NR <= 128 && NG <= 2 ? 3 : 2) void k_kv_at
     }
 }
 
-// The splits' results into the output: a row of a head by D / 4 lanes.
-template <int D>
-__global__ __launch_bounds__(256) void k_kv_join(KvArgs a, KvAttendArgs p, int rows_per_tile)
+// ---- many rows ----------------------------------------------------------------------------------
+
+typedef _Float16 f16x2_t __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+__device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi)
+{
+    const f32x2 v = {lo, hi};
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, f16x2_t));
+}
+// c * scale + zero of two codes that sit in bits 4 .. 7 of the halves of w: there a code is the fp16 number c 2^-20
+// (below fp16's normal range its patterns count in equal steps), which the scale makes good.
+__device__ __forceinline__ uint32_t dequant2(uint32_t w, uint32_t scale, uint32_t zero)
+{
+    const f16x2_t c = __builtin_bit_cast(f16x2_t, w & 0x00F000F0u);
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(c, __builtin_bit_cast(f16x2_t, scale), __builtin_bit_cast(f16x2_t, zero)));
+}
+
+// W waves of 32 rows; the keys and values of TOK tokens at a time, dequantised into LDS by all of them.
+template <int D, int NG, int W, int TOK>
+__global__ __launch_bounds__(64 * W, D == 256 ? 1 : 2) void k_kv_attend_many(KvArgs a, KvAttendArgs p)
+{
+    constexpr int KS = D / 16, DT = D / 32, TB = TOK / 32, ROWS = 32 * W, BLOCKS = TOK / 16;
+    // a wave dequantises one of PARTS parts of a block of 16 tokens: PIECES times 8 features of a key, or 2 of 4 values, a lane
+    constexpr int PARTS = W / BLOCKS, PIECES = D / 32 / PARTS, GROUPS = NG > PARTS ? NG / PARTS : 1;  // groups of a part
+    constexpr int KROW = 2 * D, VROW = 2 * TOK, KBYTES = TOK * KROW, VBYTES = D * VROW;
+    constexpr int WINDOW = 64 / BLOCKS;  // tiles whose page numbers a wave holds at a time
+    static_assert(W % BLOCKS == 0 && PIECES >= 1 && GROUPS <= 4, "parts");
+    extern __shared__ u32x4 smem_kv[];
+    uint8_t *const lds = reinterpret_cast<uint8_t *>(smem_kv);
+    __shared__ uint32_t reduced[3];
+    const uint32_t ln = threadIdx.x & 63u, c32 = ln & 31u, hh = ln >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int tile_id = p.by_splits.of(blockIdx.x), split = blockIdx.x - tile_id * p.splits, h = blockIdx.y, b = blockIdx.z;
+    const int rt = p.row_tiles - 1 - tile_id;  // (the last rows have the most keys: first)
+    KvShare w;
+    if (!kv_share<TOK>(a, p, b, rt, ROWS, w) || split >= w.live) return;
+    const int v0 = split * w.share, v1 = min(v0 + w.share, w.span.tiles);
+    const int wrow = rt * ROWS + 32 * wave;
+    const int wlo = w.base + p.by_R.of(wrow);  // the wave's first and last position
+    const int whi = w.base + p.by_R.of(min(wrow + 32, w.n_rows) - 1);
+    const bool idle = wrow >= w.n_rows;
+
+    // queries in fp16, exactly (but for elements below 2^-27 of a row's largest): each row at a power of two of its own
+    const int row = wrow + static_cast<int>(c32), rc = min(row, w.n_rows - 1), qi = p.by_R.of(rc);
+    const int pos = w.base + qi;
+    // Rows of both operands are cut into slots of 16 bytes, which lie permuted by their row's number: 16 lanes are served at once
+    // if they touch every one of 64 banks once, in reads (16 rows, one slot) and in writes (4 keys' 4 slots; 16 features' halves of
+    // one or two) alike.
+    auto key_slot = [](uint32_t t) { return D == 64 ? (((t >> 1) & 1u) << 2) | ((t >> 2) & 3u) : ((t & 3u) << 2) | ((t >> 2) & 3u); };
+    auto value_slot = [](uint32_t d) { return TOK == 64 ? (d >> 1) & 7u : (d >> 2) & 3u; };
+    u32x4 raw[KS];
+    {
+        const uint8_t *src = p.Q + (w.row0 + qi) * p.ldQ + (h * p.R + rc - qi * p.R) * (2 * D) + 16 * hh;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) raw[ks] = *reinterpret_cast<const u32x4 *>(src + 32 * ks);
+    }
+
+    const int n_blocks = (min(w.len, a.ld_table << a.lg_page) + 15) / 16;
+    const uint32_t page_len = 1u << a.lg_page, page_mask = page_len - 1u;
+    const int32_t *table = a.table + static_cast<int64_t>(b) * a.ld_table;
+    const uint8_t *const cache_h = a.cache + static_cast<int64_t>(h) * a.cell_bytes;
+    // page numbers of the WINDOW steps from v on: lane BLOCKS * step + block (-1: no page)
+    auto pages_of = [&](int v) __attribute__((always_inline)) {
+        const int block = w.span.tile(min(v + static_cast<int>(ln) / BLOCKS, v1 - 1)) * BLOCKS + static_cast<int>(ln) % BLOCKS;
+        const int id = table[(16 * min(block, n_blocks - 1)) >> a.lg_page];
+        return block < n_blocks && static_cast<uint32_t>(id) < static_cast<uint64_t>(a.n_pages) ? id : -1;
+    };
+
+    // What a lane loads of its wave's part of a tile: codes of one key and of four values, and one of the scales and zeros
+    // of each that its neighbours and it need.  Keys: lane l has quarter l % 4 of token l / 4 and group l % 4 of the part.
+    // Values: chunk m = l % 16 of the 4 tokens from 8 (l / 16 % 2) + 4 (l / 32) on, and group m / 4 of token m % 4.
+    // (No branches: the loads' order is known, and so is how many are younger than the ones waited for.)
+    struct Codes {
+        uint32_t k[PIECES], v[4], km, vm;
+    };
+    const int block = wave % BLOCKS, part = wave / BLOCKS;
+    const uint32_t m16 = ln & 15u, quad = ln & 3u, vt = 8u * ((ln >> 4) & 1u) + 4u * hh;
+    const uint32_t group0 = part * NG / PARTS, k_at = ln * (D / 8) + 4u * PIECES * part, v_at = vt * (D / 2) + (D == 64 ? m16 / 2 * 4 : D == 256 ? m16 * 8 + 4 * part : m16 * 4);
+    const uint32_t km_at = 4u * ((group0 + min(quad, GROUPS - 1u)) * page_len + (ln >> 2)), vm_at = 4u * ((NG + group0 + min(m16 >> 2, GROUPS - 1u)) * page_len + vt + (m16 & 3u));
+    // (keys of step vk, values of step vv; of steps past the last: the last's)
+    auto load_codes = [&](Codes &c, int vk, int vv, int base, int pages) __attribute__((always_inline)) {
+        const int k = min(vk, v1 - 1), v = min(vv, v1 - 1);
+        const int idk = max(__builtin_amdgcn_readlane(pages, (k - base) * BLOCKS + block), 0), idv = max(__builtin_amdgcn_readlane(pages, (v - base) * BLOCKS + block), 0);
+        const uint32_t sk = (16u * (w.span.tile(k) * BLOCKS + block)) & page_mask, sv = (16u * (w.span.tile(v) * BLOCKS + block)) & page_mask;
+        const uint8_t *ck = cache_h + idk * a.page_bytes, *cv = cache_h + idv * a.page_bytes;
+        const uint8_t *ks = ck + sk * (D / 2), *vs = cv + (page_len + sv) * (D / 2);
+        c.km = *reinterpret_cast<const uint32_t *>(ck + page_len * D + 4 * sk + km_at);
+#pragma unroll
+        for (int e = 0; e < PIECES; ++e) c.k[e] = reinterpret_cast<const uint32_t *>(ks + k_at)[e];
+        c.vm = *reinterpret_cast<const uint32_t *>(cv + page_len * D + 4 * sv + vm_at);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) c.v[i] = *reinterpret_cast<const uint32_t *>(vs + v_at + i * (D / 2));
+    };
+    int base = v0, pages = 0;
+    Codes ca = {}, cb = {};
+    if (v0 < v1) {
+        pages = pages_of(v0);
+        load_codes(ca, v0, v0, base, pages);
+        load_codes(cb, v0 + 1, v0 + 1, base, pages);
+    }
+
+    // The normalisation of keys and of values: a power of two that brings the largest among those that some row sees into
+    // 2^-3 .. 2^-2, so that scales fit fp16 times the codes' 2^20 (what is 2^12 times smaller than the largest still has
+    // fp16's 11 bits, and then one less for every halving).  From scales and zeros alone, 8 ng bytes a token and head.
+    float k_norm, v_norm, k_undo, v_undo;
+    bool absent;  // a block of 16 tokens that has no page
+    {
+        if (threadIdx.x < 3) reduced[threadIdx.x] = 0;
+        uint32_t top[2] = {0, 0}, missing = 0;
+        constexpr int U = NG <= 2 ? 4 : 2;  // tiles whose loads are in flight together
+        for (int v = v0 + wave; v < v1; v += U * W) {
+            int id[U], key[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                key[u] = w.span.tile(min(v + u * W, v1 - 1)) * TOK + static_cast<int>(ln) % TOK;
+                id[u] = table[min(key[u], 16 * n_blocks - 1) >> a.lg_page];
+            }
+            uint32_t x[U][2 * NG];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const bool exists = key[u] < 16 * n_blocks, good = static_cast<uint32_t>(id[u]) < static_cast<uint64_t>(a.n_pages);
+                missing |= exists && !good ? 1u : 0u;
+                const bool seen = exists & good & (key[u] <= w.hi) & ((p.window == 0) | (key[u] > w.lo - p.window) | (key[u] < p.sinks));
+                const uint32_t *src = reinterpret_cast<const uint32_t *>(cache_h + (good ? id[u] : 0) * a.page_bytes + page_len * D) + (static_cast<uint32_t>(key[u]) & page_mask);
+#pragma unroll
+                for (int g = 0; g < 2 * NG; ++g) x[u][g] = seen ? src[g * page_len] : 0u;
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int g = 0; g < 2 * NG; ++g) {
+                    const float z = bf16_hi_to_f32(x[u][g]), z1 = __builtin_fmaf(15.0f, bf16_lo_to_f32(x[u][g]), z);
+                    const uint32_t big = max(__float_as_uint(z) & 0x7FFFFFFFu, __float_as_uint(z1) & 0x7FFFFFFFu);
+                    top[g / NG] = max(top[g / NG], big < 0x7F800000u ? big : 0u);  // (what is not finite has no part in it)
+                }
+        }
+        __syncthreads();
+        const uint32_t kt = wave_max(top[0]), vt = wave_max(top[1]);
+        if (ln == 0) {
+            atomicMax(&reduced[0], kt);
+            atomicMax(&reduced[1], vt);
+        }
+        if (__builtin_amdgcn_ballot_w64(missing != 0) && ln == 0) atomicOr(&reduced[2], 1u);
+        __syncthreads();
+        const int ku = min(max(251 - static_cast<int>(reduced[0] >> 23), 1), 254), vu = min(max(251 - static_cast<int>(reduced[1] >> 23), 1), 254);
+        k_norm = __uint_as_float(static_cast<uint32_t>(ku) << 23);
+        v_norm = __uint_as_float(static_cast<uint32_t>(vu) << 23);
+        k_undo = __builtin_amdgcn_ldexpf(1.0f, 127 - ku);
+        v_undo = __builtin_amdgcn_ldexpf(1.0f, 127 - vu);
+        absent = reduced[2] != 0;
+    }
+
+    // (heads of 256: in LDS, laid out as the keys are; beside 128 accumulators 64 registers are too many)
+    constexpr bool q_in_lds = D == 256;
+    uint8_t *const q_row = lds + 2 * KBYTES + 2 * VBYTES + (32 * wave + c32) * KROW;
+    const uint32_t kf = key_slot(c32), vf = value_slot(c32);
+    f16x8_t q[q_in_lds ? 1 : KS];
+    float row_scale;
+    {
+        uint32_t top = 0;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) top = max(top, max((raw[ks][e] << 16) & 0x7FFFFFFFu, raw[ks][e] & 0x7FFF0000u));
+        const auto both = __builtin_amdgcn_permlane32_swap(top, top, false, false);
+        const uint32_t x = both[0], y = both[1];
+        const int up = min(max(267 - static_cast<int>(max(x, y) >> 23), 1), 254);  // times 2^(up - 127): the largest in 2^13 .. 2^14
+        const float f = __uint_as_float(static_cast<uint32_t>(up) << 23) * (p.scale < 0.0f ? -1.0f : 1.0f);
+        row_scale = fabsf(p.scale) * __builtin_amdgcn_ldexpf(1.0f, 127 - up);
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            u32x4 o;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] = pack_f16x2(bf16_lo_to_f32(raw[ks][e]) * f, bf16_hi_to_f32(raw[ks][e]) * f);
+            if (q_in_lds) *reinterpret_cast<u32x4 *>(q_row + 16 * ((2 * ks + hh) ^ kf)) = o;  // (read by this wave alone)
+            else q[ks] = __builtin_bit_cast(f16x8_t, o);
+        }
+        if (q_in_lds) wave_lds_fence();
+    }
+
+    // Scale (times the codes' 2^20) and zero in fp16, normalised.  What is larger than the normalisation knows, or not a
+    // number, is no row's: zeros, so that it stays finite next to weights of 0.
+    auto converted = [&](uint32_t x, float f) __attribute__((always_inline)) {
+        const float sc = bf16_lo_to_f32(x) * f, ze = bf16_hi_to_f32(x) * f, z1 = __builtin_fmaf(15.0f, sc, ze);
+        const bool ok = max(__float_as_uint(ze) & 0x7FFFFFFFu, __float_as_uint(z1) & 0x7FFFFFFFu) <= 0x3E800000u;
+        const uint32_t y = pack_f16x2(sc * 0x1p20f, ze);
+        return ok ? y : 0u;
+    };
+    auto store_keys = [&](const Codes &c, auto piece, int pk) __attribute__((always_inline)) {
+        constexpr int i = decltype(piece)::value, gr = NG >= PARTS ? i / (D / 32 / NG) : 0;
+        const uint32_t t = 16u * block + (ln >> 2), kk = part * PIECES + i;
+        const uint32_t mt = __builtin_amdgcn_update_dpp(0u, c.km, 0x55 * gr, 0xF, 0xF, true);  // lane gr of each four
+        const uint32_t sc = __builtin_amdgcn_perm(mt, mt, 0x01000100u), ze = __builtin_amdgcn_perm(mt, mt, 0x03020302u);
+        const uint32_t y = c.k[i];
+        const u32x4 o = {dequant2(y << 4, sc, ze), dequant2(y, sc, ze), dequant2(y >> 4, sc, ze), dequant2(y >> 8, sc, ze)};
+        *reinterpret_cast<u32x4 *>(lds + pk * KBYTES + t * KROW + 16 * ((4 * kk + quad) ^ key_slot(t))) = o;
+    };
+    const uint32_t byte0 = (D == 256 ? 0u : static_cast<uint32_t>(part * PIECES)) + (D == 64 ? 2u * (m16 & 1u) : 0u), sel0 = 0x0C000C00u | ((4u + byte0) << 16) | byte0;
+    auto store_values = [&](const Codes &c, auto piece, int pv) __attribute__((always_inline)) {
+        constexpr int i = decltype(piece)::value, lane = NG >= PARTS ? 4 * (i / (D / 32 / NG)) : 0;  // lanes 4 gr .. 4 gr + 3 of the row have the group's four tokens
+        const uint32_t chunk = 2u * block + hh, half = (ln >> 4) & 1u, sel = sel0 + i * 0x00010001u;
+        const uint32_t m0 = __builtin_amdgcn_update_dpp(0u, c.vm, 0x150 + lane, 0xF, 0xF, true), m1 = __builtin_amdgcn_update_dpp(0u, c.vm, 0x151 + lane, 0xF, 0xF, true);
+        const uint32_t m2 = __builtin_amdgcn_update_dpp(0u, c.vm, 0x152 + lane, 0xF, 0xF, true), m3 = __builtin_amdgcn_update_dpp(0u, c.vm, 0x153 + lane, 0xF, 0xF, true);
+        const uint32_t sc[2] = {__builtin_amdgcn_perm(m1, m0, 0x05040100u), __builtin_amdgcn_perm(m3, m2, 0x05040100u)};
+        const uint32_t ze[2] = {__builtin_amdgcn_perm(m1, m0, 0x07060302u), __builtin_amdgcn_perm(m3, m2, 0x07060302u)};
+        const uint32_t y0 = __builtin_amdgcn_perm(c.v[1], c.v[0], sel), y1 = __builtin_amdgcn_perm(c.v[3], c.v[2], sel);
+#pragma unroll
+        for (int odd = 0; odd < 2; ++odd) {
+            const uint32_t d = 16 * (2 * (part * PIECES + i) + odd) + m16;
+            const uint2 o = make_uint2(dequant2(odd ? y0 : y0 << 4, sc[0], ze[0]), dequant2(odd ? y1 : y1 << 4, sc[1], ze[1]));
+            *reinterpret_cast<uint2 *>(lds + 2 * KBYTES + pv * VBYTES + d * VROW + 16 * (chunk ^ value_slot(m16)) + 8 * half) = o;
+        }
+    };
+    auto store_codes = [&](Codes &c, int pk, int pv) __attribute__((always_inline)) {
+        c.km = converted(c.km, k_norm);
+        c.vm = converted(c.vm, v_norm);
+        for_each<PIECES>([&](auto piece) __attribute__((always_inline)) {
+            store_keys(c, piece, pk);
+            store_values(c, piece, pv);
+        });
+    };
+
+    f32x16 o[DT];
+    float mx = kKvLowest, l = 0.0f, k_exp = 0.0f;
+#pragma unroll
+    for (int t = 0; t < DT; ++t)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[t][e] = 0.0f;
+    const float log2e = 1.44269504f;
+    const float cap_in = p.softcap > 0.0f ? 2.0f * log2e / p.softcap : 0.0f, cap_out = p.softcap * log2e;
+
+    // where a lane reads its rows of the two operands (par: which of the two buffers)
+    auto key_at = [&](int par, int i) __attribute__((always_inline)) {  // i = tb * KS + k
+        return __builtin_bit_cast(f16x8_t, *reinterpret_cast<const u32x4 *>(lds + par * KBYTES + (32 * (i / KS) + c32) * KROW + 16 * ((2 * (i % KS) + hh) ^ kf)));
+    };
+    auto value_at = [&](int par, int j) __attribute__((always_inline)) {  // j = step of 16 tokens * DT + t
+        return __builtin_bit_cast(f16x8_t, *reinterpret_cast<const u32x4 *>(lds + 2 * KBYTES + par * VBYTES + (32 * (j % DT) + c32) * VROW + 16 * ((2 * (j / DT) + hh) ^ vf)));
+    };
+    constexpr int NQ = TB * KS, NP = 2 * TB * DT, NS = 16 * TB;  // products with keys, with values; scores of a lane
+    uint32_t pw[NS / 2];                                         // weights, in the order in which the products take them
+
+    auto query_at = [&](int i) __attribute__((always_inline)) {
+        if constexpr (q_in_lds) return __builtin_bit_cast(f16x8_t, *reinterpret_cast<const u32x4 *>(q_row + 16 * ((2 * (i % KS) + hh) ^ kf)));
+        else return q[i % KS];
+    };
+    auto score = [&](f32x16 (&acc)[TB], const f16x8_t &key, const f16x8_t &query, int i) __attribute__((always_inline)) {
+        const f32x16 zero = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
+        acc[i / KS] = __builtin_amdgcn_mfma_f32_32x32x16_f16(key, query, i % KS ? acc[i / KS] : zero, 0, 0, 0);
+    };
+    auto value = [&](const f16x8_t &val, int j) __attribute__((always_inline)) {
+        const int first = 4 * (j / DT);
+        const f16x8_t pb = __builtin_bit_cast(f16x8_t, (u32x4{pw[first], pw[first + 1], pw[first + 2], pw[first + 3]}));
+        o[j % DT] = __builtin_amdgcn_mfma_f32_32x32x16_f16(val, pb, o[j % DT], 0, 0, 0);
+    };
+    // all of a tile's scores, all of its values: operands read ahead
+    auto all_scores = [&](f32x16 (&acc)[TB], int par) __attribute__((always_inline)) {
+        constexpr int A = q_in_lds ? 2 : 4;
+        f16x8_t fr[A + 1], fq[A + 1];
+#pragma unroll
+        for (int i = 0; i < A; ++i) {
+            fr[i] = key_at(par, i);
+            fq[i] = query_at(i);
+        }
+#pragma unroll
+        for (int i = 0; i < NQ; ++i) {
+            if (i + A < NQ) {
+                fr[(i + A) % (A + 1)] = key_at(par, i + A);
+                fq[(i + A) % (A + 1)] = query_at(i + A);
+            }
+            score(acc, fr[i % (A + 1)], fq[i % (A + 1)], i);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    auto all_values = [&](int par) __attribute__((always_inline)) {
+        constexpr int A = q_in_lds ? 2 : 4;
+        f16x8_t fr[A + 1];
+#pragma unroll
+        for (int j = 0; j < A; ++j) fr[j] = value_at(par, j);
+#pragma unroll
+        for (int j = 0; j < NP; ++j) {
+            if (j + A < NP) fr[(j + A) % (A + 1)] = value_at(par, j + A);
+            value(fr[j % (A + 1)], j);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    auto take = [&](float (&s)[NS], const f32x16 (&acc)[TB]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < NS; ++i) s[i] = acc[i / 16][i % 16];
+    };
+    auto exp_pair = [&](float (&s)[NS], int i) __attribute__((always_inline)) {  // in the scores' place
+        s[2 * i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[2 * i], k_exp, -mx));
+        s[2 * i + 1] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[2 * i + 1], k_exp, -mx));
+        asm volatile("" : "+v"(s[2 * i]), "+v"(s[2 * i + 1]));  // (here, not where they are needed)
+    };
+    auto pack_pair = [&](const float (&s)[NS], int i) __attribute__((always_inline)) {  // (the sum takes the weights as the products do)
+        pw[i] = pack_f16x2(s[2 * i], s[2 * i + 1]);
+        l = __builtin_amdgcn_fdot2(__builtin_bit_cast(f16x2_t, pw[i]), __builtin_bit_cast(f16x2_t, 0x3C003C00u), l, false);
+        asm volatile("" : "+v"(pw[i]), "+v"(l));
+    };
+    // The running maximum brought up to a tile's.  Weights reach 2^14: 2^6 where the maximum has just been taken, and a maximum
+    // follows past 2^8 of that only.
+    auto settle = [&](float top) __attribute__((always_inline)) {
+        if (__builtin_amdgcn_ballot_w64(top > kKvLowest && top * k_exp > mx + 14.0f) == 0) return;
+        const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
+        const float both = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+        const float now = both > kKvLowest ? fmaxf(mx, both * k_exp - 6.0f) : mx, alpha = __builtin_amdgcn_exp2f(mx - now);
+        mx = now;
+        l *= alpha;
+#pragma unroll
+        for (int t = 0; t < DT; ++t) o[t] *= alpha;
+    };
+
+    // Step by step: the keys of tile i + 2 and the values of i + 1 are dequantised while tile i is worked on, from codes that
+    // were loaded two steps before (two sets in turn).
+    if (v0 < v1) {
+        store_codes(ca, 0, 0);
+        cb.km = converted(cb.km, k_norm);
+        for_each<PIECES>([&](auto piece) __attribute__((always_inline)) { store_keys(cb, piece, 1); });  // of the second tile
+        load_codes(ca, v0 + 2, v0 + 1, base, pages);
+        load_codes(cb, v0 + 3, v0 + 2, base, pages);
+        __syncthreads();
+
+        auto begin = [&](int v) __attribute__((always_inline)) {
+            if (v + 4 - base >= WINDOW) {
+                base = v;
+                pages = pages_of(v);
+            }
+        };
+        // tiles that every row of the workgroup sees whole: steps f0 .. f1 - 1 (but for absent blocks, and for bounded scores)
+        const int tile0 = p.window > 0 && w.hi - p.window >= 0 ? (w.hi - p.window) / TOK + 1 : 0, tile1 = w.lo < 0 ? 0 : (w.lo + 1) / TOK;
+        const int f0 = max(max(v0, w.span.first), w.span.first + tile0 - w.span.start);
+        const int f1 = p.softcap > 0.0f || absent ? 0 : min(v1, w.span.first + tile1 - w.span.start);
+        const float scale2 = row_scale * k_undo;
+
+        for (int v = v0; v < v1;) {
+            if (((v - v0) & 1) == 0 && v >= f0 && v + 2 < f1) {
+                // Two tiles a round.  While the weights of a tile are made of its scores, the products that give the next tile's
+                // run in the matrix cores; while its values are multiplied, the next maximum is looked for and codes
+                // are dequantised.  A slice is one product and the vector instructions of about its time (the order is
+                // pinned); operands are read slices ahead.
+                float sa[NS], sb[NS], top;
+                k_exp = scale2 * log2e;
+                {
+                    f32x16 acc[TB];
+                    all_scores(acc, 0);
+                    take(sa, acc);
+                    top = sa[0];
+#pragma unroll
+                    for (int i = 1; i < NS; ++i) top = fmaxf(top, sa[i]);
+                    __syncthreads();
+                }
+                auto fused = [&](auto parity, float (&s)[NS], float (&next)[NS], Codes &codes, int v) __attribute__((always_inline)) {
+                    constexpr int P = decltype(parity)::value, Q = P ^ 1, QP = NS / 2 * 3 / 4, R = NS / 2 - QP, H = TB == 1 ? NP / 4 : NP / 2, M = NP / 2;
+                    static_assert(H < NP - DT, "the last weights are packed before the slices that take them");
+                    constexpr int A = q_in_lds ? 2 : 3;  // slices that operands are read ahead
+                    begin(v);
+                    settle(top);
+                    __builtin_amdgcn_sched_barrier(0);
+                    f32x16 acc[TB];
+                    f16x8_t fr[A + 1], fq[A + 1];
+#pragma unroll
+                    for (int i = 0; i < A; ++i) {
+                        fr[i] = key_at(Q, i);
+                        fq[i] = query_at(i);
+                    }
+                    for_each<NQ>([&](auto ii) __attribute__((always_inline)) {
+                        constexpr int i = decltype(ii)::value;
+                        fr[(i + A) % (A + 1)] = i + A < NQ ? key_at(Q, i + A) : value_at(P, i + A - NQ);
+                        if constexpr (i + A < NQ) fq[(i + A) % (A + 1)] = query_at(i + A);
+                        score(acc, fr[i % (A + 1)], fq[i % (A + 1)], i);
+#pragma unroll
+                        for (int x = i * QP / NQ; x < (i + 1) * QP / NQ; ++x) exp_pair(s, x);
+#pragma unroll
+                        for (int x = i == 0 ? 0 : (i - 1) * QP / NQ; x < i * QP / NQ; ++x) pack_pair(s, x);
+                        __builtin_amdgcn_sched_barrier(0);
+                    });
+                    take(next, acc);
+                    for_each<NP>([&](auto jj) __attribute__((always_inline)) {
+                        constexpr int j = decltype(jj)::value;
+                        if constexpr (j == 0) {
+#pragma unroll
+                            for (int x = (NQ - 1) * QP / NQ; x < QP; ++x) pack_pair(s, x);
+                        }
+                        if constexpr (j + A < NP) fr[(NQ + j + A) % (A + 1)] = value_at(P, j + A);
+                        value(fr[(NQ + j) % (A + 1)], j);
+                        if constexpr (j < H) {
+#pragma unroll
+                            for (int x = QP + j * R / H; x < QP + (j + 1) * R / H; ++x) exp_pair(s, x);
+                        }
+                        if constexpr (j > 0 && j <= H) {
+#pragma unroll
+                            for (int x = QP + (j - 1) * R / H; x < QP + j * R / H; ++x) pack_pair(s, x);
+                        }
+                        if constexpr (j >= M) {
+#pragma unroll
+                            for (int x = (j - M) * NS / (NP - M); x < (j - M + 1) * NS / (NP - M); ++x) top = x == 0 ? next[0] : fmaxf(top, next[x]);
+                            asm volatile("" : "+v"(top));
+                        }
+                        constexpr int S = NP / 4;  // (the first quarter is left to the codes' last delay)
+                        if constexpr (j == S - 1) {
+                            codes.km = converted(codes.km, k_norm);
+                            codes.vm = converted(codes.vm, v_norm);
+                        }
+                        for_each<PIECES>([&](auto piece) __attribute__((always_inline)) {
+                            constexpr int x = decltype(piece)::value;
+                            if constexpr (S + 2 * x * (NP - S) / (2 * PIECES) == j) store_keys(codes, piece, P);
+                            if constexpr (S + (2 * x + 1) * (NP - S) / (2 * PIECES) == j) store_values(codes, piece, Q);
+                        });
+                        __builtin_amdgcn_sched_barrier(0);
+                    });
+                    load_codes(codes, v + 4, v + 3, base, pages);
+                    __syncthreads();
+                };
+                do {
+                    fused(std::integral_constant<int, 0>{}, sa, sb, ca, v);
+                    fused(std::integral_constant<int, 1>{}, sb, sa, cb, v + 1);
+                    v += 2;
+                } while (v + 2 < f1);
+                // the last one, whose scores are there
+                begin(v);
+                settle(top);
+#pragma unroll
+                for (int i = 0; i < NS / 2; ++i) exp_pair(sa, i);
+#pragma unroll
+                for (int i = 0; i < NS / 2; ++i) pack_pair(sa, i);
+            } else {
+                // any tile: bounded scores, hidden keys
+                begin(v);
+                const int t0 = w.span.tile(v) * TOK, par = (v - v0) & 1;
+                const bool active = !idle && t0 <= whi && (p.window == 0 || t0 + TOK > wlo - p.window + 1 || t0 < p.sinks);
+                if (active) {
+                    f32x16 acc[TB];
+                    all_scores(acc, par);
+                    k_exp = scale2 * (p.softcap > 0.0f ? 1.0f : log2e);
+                    float s[NS], top = kKvLowest;
+                    take(s, acc);
+                    if (p.softcap > 0.0f) {
+#pragma unroll
+                        for (int i = 0; i < NS; ++i) {
+                            const float y = __builtin_amdgcn_exp2f(s[i] * (k_exp * cap_in)) + 1.0f;
+                            s[i] = __builtin_fmaf(-2.0f * cap_out, __builtin_amdgcn_rcpf(y), cap_out);
+                        }
+                        k_exp = 1.0f;
+                    }
+                    const int from = t0 + 4 * static_cast<int>(hh), below = pos - from, low = p.window > 0 ? below - p.window : -(1 << 30), first = p.sinks - from;
+#pragma unroll
+                    for (int i = 0; i < NS; ++i) {
+                        const int key = 8 * (i >> 2) + (i & 3);  // (after the lane's first)
+                        s[i] = (key <= below) & ((key > low) | (key < first)) ? s[i] : kKvLowest;
+                    }
+                    if (absent) {
+                        const uint32_t bad = static_cast<uint32_t>(__builtin_amdgcn_ballot_w64(pages < 0) >> ((v - base) * BLOCKS));
+#pragma unroll
+                        for (int i = 0; i < NS; ++i) s[i] = (bad >> (i >> 3)) & 1u ? kKvLowest : s[i];
+                    }
+#pragma unroll
+                    for (int i = 0; i < NS; ++i) top = fmaxf(top, s[i]);
+                    settle(top);
+#pragma unroll
+                    for (int i = 0; i < NS; ++i) s[i] = s[i] > kKvLowest ? __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], k_exp, -mx)) : 0.0f;
+#pragma unroll
+                    for (int i = 0; i < NS / 2; ++i) pack_pair(s, i);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < NS / 2; ++i) pw[i] = 0;
+                }
+                __syncthreads();  // (the keys' buffer is the next one's)
+            }
+            const int par = (v - v0) & 1;
+            all_values(par);
+            if (par) {
+                store_codes(cb, 1, 0);
+                load_codes(cb, v + 4, v + 3, base, pages);
+            } else {
+                store_codes(ca, 0, 1);
+                load_codes(ca, v + 4, v + 3, base, pages);
+            }
+            __syncthreads();
+            ++v;
+        }
+    }
+
+    {
+        const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
+        l = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    }
+    if (row >= w.n_rows) return;
+    if (w.live == 1) {
+        uint8_t *dst = p.out + (w.row0 + qi) * p.ldOut + (h * p.R + row - qi * p.R) * (2 * D) + 8 * hh;
+        const float inv = l > 0.0f ? v_undo / l : 0.0f;
+#pragma unroll
+        for (int t = 0; t < DT; ++t)
+#pragma unroll
+            for (int e = 0; e < 16; e += 4)
+                *reinterpret_cast<uint2 *>(dst + 64 * t + 4 * e) =
+                    make_uint2(pack_bf16x2(o[t][e] * inv, o[t][e + 1] * inv), pack_bf16x2(o[t][e + 2] * inv, o[t][e + 3] * inv));
+    } else {
+        const int64_t at = (((static_cast<int64_t>(b) * a.heads + h) * p.row_tiles + rt) * p.splits + split) * ROWS + (row - rt * ROWS);
+        float *dst = p.part + at * D + 4 * hh;
+        const float f = v_undo;
+#pragma unroll
+        for (int t = 0; t < DT; ++t)
+#pragma unroll
+            for (int e = 0; e < 16; e += 4)
+                *reinterpret_cast<f32x4 *>(dst + 32 * t + 2 * e) = f32x4{o[t][e] * f, o[t][e + 1] * f, o[t][e + 2] * f, o[t][e + 3] * f};
+        if (hh == 0) *reinterpret_cast<float2 *>(p.part_ml + 2 * at) = make_float2(mx, l);
+    }
+}
+
+// The splits' results into the output: a row of a head by D / 4 lanes.  Every split's maximum and sum first, then the
+// accumulators, eight splits' loads at a time: one after the other they would be as many latencies (43 splits: 22.8 us).
+template <int D, int TOK>
+__global__ __launch_bounds__(256) void k_kv_join(KvArgs a, KvAttendArgs p, int rows)
 {
     constexpr int LPR = D / 4, RPW = 256 / LPR;
     const int h = blockIdx.y, b = blockIdx.z, c = threadIdx.x % LPR;
-    const int row = blockIdx.x * RPW + threadIdx.x / LPR;
-    int64_t row0;
-    int n, len;
-    if (!kv_sequence(a, b, row0, n, len)) return;
-    const int n_rows = min(n, a.max_new) * p.R;
-    if (row >= n_rows) return;
-    const int rt = row / rows_per_tile, base = len - n;
-    const int lo = base + rt * rows_per_tile / p.R, hi = base + (min((rt + 1) * rows_per_tile, n_rows) - 1) / p.R;
-    const KvSpan span = kv_span(a, p.window, p.sinks, lo, hi, len);
-    const int live = kv_live(span.tiles, kv_share(span.tiles, p.splits));
-    if (live == 1) return;
-    const int64_t at = (((static_cast<int64_t>(b) * a.heads + h) * p.row_tiles + rt) * p.splits) * rows_per_tile + (row - rt * rows_per_tile);
+    const int row = blockIdx.x * RPW + threadIdx.x / LPR, rt = row / rows;
+    KvShare w;
+    if (!kv_share<TOK>(a, p, b, rt, rows, w) || row >= w.n_rows || w.live == 1) return;
+    const int64_t at = (((static_cast<int64_t>(b) * a.heads + h) * p.row_tiles + rt) * p.splits) * rows + (row - rt * rows);
+    const float *part = p.part + at * D + 4 * c;
+    const float2 *ml = reinterpret_cast<const float2 *>(p.part_ml) + at;
     float mx = kKvLowest, l = 0.0f;
     f32x4 o = {0, 0, 0, 0};
-    for (int s = 0; s < live; ++s) {
-        const int64_t r = at + static_cast<int64_t>(s) * rows_per_tile;
-        const float2 ml = *reinterpret_cast<const float2 *>(p.part_ml + 2 * r);
-        const f32x4 x = *reinterpret_cast<const f32x4 *>(p.part + r * D + 4 * c);
-        const float now = fmaxf(mx, ml.x), f1 = __builtin_amdgcn_exp2f(mx - now), f2 = __builtin_amdgcn_exp2f(ml.x - now);
+    for (int s = 0; s < w.live; s += 8) {
+        float2 x[8];
+        f32x4 y[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            const int64_t r = static_cast<int64_t>(min(s + u, w.live - 1)) * rows;
+            x[u] = ml[r];
+            y[u] = *reinterpret_cast<const f32x4 *>(part + r * D);
+        }
+        float now = mx;
+#pragma unroll
+        for (int u = 0; u < 8; ++u) now = fmaxf(now, x[u].x);
+        const float f = __builtin_amdgcn_exp2f(mx - now);
         mx = now;
-        l = l * f1 + ml.y * f2;
-        o = o * f1 + x * f2;
+        l *= f;
+        o *= f;
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            const float g = s + u < w.live ? __builtin_amdgcn_exp2f(x[u].x - now) : 0.0f;
+            l += x[u].y * g;
+            o += y[u] * g;
+        }
     }
     const float inv = l > 0.0f ? 1.0f / l : 0.0f;
-    const int i = row / p.R;
-    uint8_t *dst = p.out + (row0 + i) * p.ldOut + (h * p.R + row - i * p.R) * (2 * D) + 8 * c;
+    const int i = p.by_R.of(row);
+    uint8_t *dst = p.out + (w.row0 + i) * p.ldOut + (h * p.R + row - i * p.R) * (2 * D) + 8 * c;
     *reinterpret_cast<uint2 *>(dst) = make_uint2(pack_bf16x2(o[0] * inv, o[1] * inv), pack_bf16x2(o[2] * inv, o[3] * inv));
 }
 
 // ---- host -----------------------------------------------------------------------------------
 
 struct KvChoice {
-    int rows, row_tiles, splits;
+    bool many;
+    int rows, row_tiles, splits, min_tiles;
 };
 
 static KvChoice choose(const KvArgs &a, int D, int R, int max_len, int compute_units)
 {
     KvChoice c;
-    c.rows = D <= 128 && a.ng == 1 && a.max_new * R > 16 ? 32 : 16;
-    c.row_tiles = (a.max_new * R + c.rows - 1) / c.rows;
-    const int64_t tiles = (max_len + kKvTile - 1) / kKvTile + 1, groups = static_cast<int64_t>(a.n_seqs) * a.heads * c.row_tiles;
-    const int64_t want = (4ll * compute_units + groups - 1) / groups;
-    c.splits = static_cast<int>(std::min<int64_t>(std::max<int64_t>(std::min(want, tiles / kKvMinTiles), 1), 256));
+    const int most = a.max_new * R;  // rows of a head and sequence
+    c.many = most > 32;
+    c.rows = c.many ? 128 : most > 16 && D <= 128 && a.ng == 1 ? 32 : 16;
+    if (c.many && D <= 128) {
+        const int64_t big = std::min<int64_t>(static_cast<int64_t>(a.n_seqs) * ((most + 255) / 256), a.rows * R / 256 + a.n_seqs);
+        if (a.heads * big >= compute_units && a.rows * R >= 512ll * a.n_seqs) c.rows = 256;
+    }
+    c.row_tiles = (most + c.rows - 1) / c.rows;
+    const int tok = !c.many ? kKvTile : D == 256 ? 32 : 64;
+    c.min_tiles = 128 * (c.many ? 2 : 1) / tok;
+    // workgroups without a split: no more than the rows there are and one more of each sequence
+    const int64_t groups = a.heads * std::min<int64_t>(static_cast<int64_t>(a.n_seqs) * c.row_tiles, a.rows * R / c.rows + a.n_seqs);
+    const int64_t tiles = (max_len + tok - 1) / tok + 1;
+    const int64_t slots = (c.many ? 1 : 3) * compute_units;
+    const int64_t want = slots / std::max<int64_t>(groups, 1);
+    c.splits = static_cast<int>(std::min<int64_t>(std::max<int64_t>(std::min(want, tiles / c.min_tiles), 1), 256));
     return c;
+}
+
+static size_t partial_rows(const KvArgs &a, const KvChoice &c)
+{
+    return static_cast<size_t>(a.n_seqs) * a.heads * c.row_tiles * c.splits * c.rows;
 }
 
 size_t kv_attend_workspace_bytes(const KvArgs &a, int D, int R, int max_len)
@@ -485,8 +1050,7 @@ size_t kv_attend_workspace_bytes(const KvArgs &a, int D, int R, int max_len)
     int cu;
     if (compute_units_of_current_device(&cu) != hipSuccess) return 0;
     const KvChoice c = choose(a, D, R, max_len, cu);
-    if (c.splits == 1) return 16;
-    return static_cast<size_t>(a.n_seqs) * a.heads * c.row_tiles * c.splits * c.rows * (D + 2) * sizeof(float);
+    return c.splits == 1 ? 16 : partial_rows(a, c) * (D + 2) * sizeof(float);
 }
 
 template <int D>
@@ -500,24 +1064,74 @@ static auto few_kernel(int ng)
     }
 }
 
+// Two tiles of keys and of values, heads of 256 their queries too: more than the default limit of LDS, allowed once per device.
+template <int D, int NG, int W, int TOK>
+static hipError_t launch_many(const KvArgs &a, const KvAttendArgs &p, dim3 grid, hipStream_t s)
+{
+    constexpr int bytes = 2 * 2 * TOK * 2 * D + (D == 256 ? 32 * W * 2 * D : 0);
+    static std::atomic<uint64_t> allowed;
+    int dev = 0;
+    hipError_t e = hipGetDevice(&dev);
+    if (e != hipSuccess) return e;
+    const uint64_t bit = dev < 64 ? 1ull << dev : 0ull;
+    if (!(allowed.load(std::memory_order_relaxed) & bit)) {
+        e = hipFuncSetAttribute(reinterpret_cast<const void *>(k_kv_attend_many<D, NG, W, TOK>), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+        if (e != hipSuccess) return e;
+        allowed.fetch_or(bit, std::memory_order_relaxed);
+    }
+    launch_kernel(k_kv_attend_many<D, NG, W, TOK>, grid, dim3(64 * W), bytes, s, a, p);
+    return hipSuccess;
+}
+
+template <int D, int W, int TOK>
+static hipError_t launch_many_of(const KvArgs &a, const KvAttendArgs &p, dim3 grid, hipStream_t s)
+{
+    switch (a.ng) {
+    case 1: return launch_many<D, 1, W, TOK>(a, p, grid, s);
+    case 2: return launch_many<D, 2, W, TOK>(a, p, grid, s);
+    case 4: return launch_many<D, D >= 128 ? 4 : 2, W, TOK>(a, p, grid, s);
+    default: return launch_many<D, D >= 256 ? 8 : 2, W, TOK>(a, p, grid, s);
+    }
+}
+
+template <int D, int TOK>
+static void launch_join(const KvArgs &a, const KvAttendArgs &p, const KvChoice &c, hipStream_t s)
+{
+    constexpr int per = 256 / (D / 4);
+    const dim3 grid((a.max_new * p.R + per - 1) / per, a.heads, a.n_seqs);
+    if (c.many) hipLaunchKernelGGL((k_kv_join<D, TOK>), grid, dim3(256), 0, s, a, p, c.rows);
+    else hipLaunchKernelGGL((k_kv_join<D, kKvTile>), grid, dim3(256), 0, s, a, p, c.rows);
+}
+
 int launch_kv_attend(const KvArgs &a, KvAttendArgs p, int D, int max_len, void *workspace, hipStream_t s)
 {
     int cu;
-    const hipError_t e = compute_units_of_current_device(&cu);
+    hipError_t e = compute_units_of_current_device(&cu);
     if (e != hipSuccess) return hip_result(e);
     const KvChoice c = choose(a, D, p.R, max_len, cu);
     p.splits = c.splits;
+    p.by_R = KvDivisor(p.R);
+    p.by_splits = KvDivisor(c.splits);
     p.row_tiles = c.row_tiles;
+    p.min_tiles = c.min_tiles;
     p.part = static_cast<float *>(workspace);
-    p.part_ml = p.part + static_cast<size_t>(a.n_seqs) * a.heads * c.row_tiles * c.splits * c.rows * D;
-    const auto kernel = D == 256 ? few_kernel<256>(a.ng)
-                        : c.rows == 32 ? (D == 64 ? k_kv_attend_few<64, 1, 2> : k_kv_attend_few<128, 1, 2>)
-                                       : (D == 64 ? few_kernel<64>(a.ng) : few_kernel<128>(a.ng));
-    launch_kernel(kernel, dim3(static_cast<uint32_t>(c.splits) * c.row_tiles, a.heads, a.n_seqs), dim3(256), 0, s, a, p);
+    p.part_ml = p.part + partial_rows(a, c) * D;
+    const dim3 grid(static_cast<uint32_t>(c.splits) * c.row_tiles, a.heads, a.n_seqs);
+    if (c.many) {
+        e = D == 256 ? launch_many_of<256, 4, 32>(a, p, grid, s)
+            : c.rows == 256 ? (D == 64 ? launch_many_of<64, 8, 64>(a, p, grid, s) : launch_many_of<128, 8, 64>(a, p, grid, s))
+                            : (D == 64 ? launch_many_of<64, 4, 64>(a, p, grid, s) : launch_many_of<128, 4, 64>(a, p, grid, s));
+        if (e != hipSuccess) return hip_result(e);
+    } else {
+        const auto kernel = D == 256 ? few_kernel<256>(a.ng)
+                            : c.rows == 32 ? (D == 64 ? k_kv_attend_few<64, 1, 2> : k_kv_attend_few<128, 1, 2>)
+                                           : (D == 64 ? few_kernel<64>(a.ng) : few_kernel<128>(a.ng));
+        launch_kernel(kernel, grid, dim3(256), 0, s, a, p);
+    }
     if (c.splits > 1) {
-        const int per = 256 / (D / 4);
-        const auto join = D == 64 ? k_kv_join<64> : D == 128 ? k_kv_join<128> : k_kv_join<256>;
-        hipLaunchKernelGGL(join, dim3((a.max_new * p.R + per - 1) / per, a.heads, a.n_seqs), dim3(256), 0, s, a, p, c.rows);
+        if (D == 64) launch_join<64, 64>(a, p, c, s);
+        else if (D == 128) launch_join<128, 64>(a, p, c, s);
+        else launch_join<256, 32>(a, p, c, s);
     }
     return hip_result(hipGetLastError());
 }
