@@ -59,10 +59,11 @@ struct KvAttendArgs {
     float *part;         // partial results: accumulators, then their maxima and sums
     float *part_ml;
     int32_t R;           // query heads per key/value head
-    KvDivisor by_R, by_splits;
+    KvDivisor by_R, by_rows, by_heads, by_splits;  // (rows: of a tile)
     int32_t window, sinks;
     float scale, softcap;
-    int32_t splits, row_tiles, min_tiles;  // shares of a row tile's steps, row tiles of a sequence, least steps of a share
+    int32_t splits;      // 1: no tile of rows is cut; with one sequence: shares of a tile's steps
+    int32_t items, row_tiles, min_tiles;  // items of a head, most tiles of rows of a sequence, least steps of a share
 };
 
 // A sequence's new rows and its length; false: its starts are no range of rows.

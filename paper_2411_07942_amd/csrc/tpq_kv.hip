@@ -188,7 +188,7 @@ __global__ __launch_bounds__(256) void k_kv_read(KvArgs a, KvReadArgs p)
 static dim3 unit_grid(const KvArgs &a, int units, int D)
 {
     const int per = 256 / (D / 8);
-    return dim3(static_cast<uint32_t>((static_cast<int64_t>(a.max_new) * units + per - 1) / per), a.n_seqs);
+    return dim3(static_cast<uint32_t>((std::min<int64_t>(a.max_new, a.rows) * units + per - 1) / per), a.n_seqs);
 }
 
 int launch_kv_append(const KvArgs &a, const KvAppendArgs &p, int D, hipStream_t s)

@@ -15,6 +15,7 @@ typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kKvTile = 32;            // tokens of a step of a wave (few rows)
+constexpr int64_t kKvMaxItems = (1ll << 32) / 512 - 1;  // (a launch has fewer than 2^32 threads)
 constexpr float kKvLowest = -3.0e38f;  // the running maximum before the first score
 
 // The steps that rows at positions lo .. hi go through: the tiles that hold visible first tokens, then those from the first
@@ -38,38 +39,157 @@ __device__ __forceinline__ KvSpan kv_span(const KvArgs &a, const KvAttendArgs &p
     return s;
 }
 
-// A workgroup's rows: a tile of `rows` of a sequence's rows of a key/value head (row i R + r: query head r of new token
-// i), and a share of the steps that they go through.  Every tile of a sequence has shares of one size, that of its last
-// tile cut into `splits`.
-struct KvShare {
+// A sequence's rows of a key/value head in tiles of `rows` (row i R + r: query head r of new token i).
+struct KvSeq {
+    int row0, n, base, len;  // first row of the tensors, new tokens (at most max_new), position of the first, tokens
+    int row_tiles, most;     // tiles of rows (0: none), steps of the last of them
+};
+template <int TOK>
+__device__ __forceinline__ KvSeq kv_seq(const KvArgs &a, const KvAttendArgs &p, int rows, int b)
+{
+    KvSeq q = {0, 0, 0, 0, 0, 0};
     int64_t row0;
+    if (b >= a.n_seqs || !kv_sequence(a, b, row0, q.n, q.len)) return q;
+    q.row0 = static_cast<int>(row0);
+    q.base = q.len - q.n;
+    q.n = min(q.n, a.max_new);
+    if (q.n == 0) return q;
+    const int last = p.by_rows.of(q.n * p.R - 1);
+    q.row_tiles = last + 1;
+    q.most = kv_span<TOK>(a, p, q.base + p.by_R.of(last * rows), q.base + q.n - 1, q.len).tiles;
+    return q;
+}
+
+// Inclusive sums along the 64 lanes: within rows of 16, then the rows' totals handed on.
+__device__ __forceinline__ uint32_t wave_scan(uint32_t v)
+{
+    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);
+    return v;
+}
+__device__ __forceinline__ uint32_t wave_total(uint32_t v) { return __builtin_amdgcn_readlane(wave_scan(v), 63); }
+
+// A workgroup's item: a tile of a sequence's rows and a share of the steps that they go through.  A head's items lie in one
+// list, sequence by sequence and tile by tile, so that no workgroup is without work: one that finds none still costs 11 ns of
+// the launch.  With several sequences the list's length is given and the largest share sought that fits it: long sequences are
+// cut into more shares than short ones (16 drafts of 5 over 300 to 9000 tokens, 8 heads: 64 us with as many shares for each, 41 with this).
+// Every tile of a sequence has shares of one size, that of its last tile.
+struct KvShare {
+    int b, rt, split;
+    int64_t row0, item0;    // the tensors' row of the sequence's first, the tile's first item
     int n_rows, base, len;  // rows of the sequence and head, position of row 0, tokens
     int lo, hi;             // first and last position among the tile's rows
     KvSpan span;
     int live, share;        // shares that have steps (at least one), steps of a share
 };
+// item >= 0: that item's.  item < 0: of tile s.rt of sequence s.b.  All lanes of the wave take part; the answer is the same in all.
 template <int TOK>
-__device__ __forceinline__ bool kv_share(const KvArgs &a, const KvAttendArgs &p, int b, int rt, int rows, KvShare &s)
+__device__ __forceinline__ bool kv_share(const KvArgs &a, const KvAttendArgs &p, int rows, int item, KvShare &s)
 {
-    int n;
-    if (!kv_sequence(a, b, s.row0, n, s.len)) return false;
-    s.base = s.len - n;
-    n = min(n, a.max_new);
-    s.n_rows = n * p.R;
-    if (rt * rows >= s.n_rows) return false;
-    s.lo = s.base + p.by_R.of(rt * rows);
-    s.hi = s.base + p.by_R.of(min((rt + 1) * rows, s.n_rows) - 1);
-    s.span = kv_span<TOK>(a, p, s.lo, s.hi, s.len);
+    const int lane = threadIdx.x & 63;
+    const bool cut = p.splits > 1;
+    KvSeq q;
+    int cuts = 1, first = 0;
+    if (a.n_seqs == 1 || (!cut && p.row_tiles == 1)) {  // as many items for each tile
+        cuts = p.splits;
+        if (item >= 0) s.b = a.n_seqs == 1 ? 0 : item;
+        q = kv_seq<TOK>(a, p, rows, s.b);
+        first = a.n_seqs == 1 ? 0 : s.b;
+    } else {
+        const KvSeq mine = kv_seq<TOK>(a, p, rows, lane);
+        const auto at = [&](int c) { return c == 0 ? mine : kv_seq<TOK>(a, p, rows, c + lane); };
+        uint32_t step = 1u << 30;
+        const auto items_of = [&](const KvSeq &x) { return x.row_tiles * max((x.most + step - 1) / step, 1u); };
+        if (cut) {
+            uint32_t total = 0, tiles = 0;  // (both below 2^31: a lane's share of them is cut off at 2^25)
+            const uint32_t most = (1u << 25) - 1u;
+            for (int c = 0; c < a.n_seqs; c += 64) {
+                const KvSeq x = at(c);
+                total = min(total + static_cast<uint32_t>(min(static_cast<uint64_t>(x.most) * x.row_tiles, static_cast<uint64_t>(most))), most);
+                tiles += x.row_tiles;
+            }
+            const bool countable = !__builtin_amdgcn_ballot_w64(total == most);  // (else: no tile is cut)
+            total = wave_total(total);
+            tiles = wave_total(tiles);
+            // as few steps a share as fit: nearly total / items, at most total / (items - tiles)
+            const uint32_t items = p.items;
+            const uint32_t ideal = (total + items - 1) / items, sure = total / (items > tiles ? items - tiles : 1u) + 1;
+            const auto fits = [&](uint32_t by) {
+                step = by;
+                uint32_t n = 0;
+                for (int c = 0; c < a.n_seqs; c += 64) n += items_of(at(c));
+                return wave_total(n) <= items;
+            };
+            if (countable) {
+                uint32_t least = max(ideal, static_cast<uint32_t>(p.min_tiles)), good = max(sure, least);
+                if (fits(least)) good = least;
+                while (good - least > least >> 4) {
+                    const uint32_t mid = least + ((good - least) >> 1);
+                    if (mid == least) break;
+                    if (fits(mid)) good = mid;
+                    else least = mid;
+                }
+                step = good;
+            }
+        }
+        if (item < 0) {
+            q = kv_seq<TOK>(a, p, rows, s.b);
+            const int end = s.b;
+            uint32_t n = 0;
+            for (int c = 0; c < end; c += 64) n += c + lane < end ? items_of(at(c)) : 0u;
+            first = wave_total(n);
+        } else {
+            bool found = false;
+            uint32_t before = 0;
+            for (int c = 0; c < a.n_seqs; c += 64) {
+                const KvSeq x = at(c);
+                const uint32_t n = items_of(x), sum = wave_scan(n) + before;
+                const uint64_t past = __builtin_amdgcn_ballot_w64(static_cast<uint32_t>(item) < sum);
+                if (past) {
+                    const int l = __builtin_ctzll(past);
+                    q.row0 = __builtin_amdgcn_readlane(x.row0, l);
+                    q.n = __builtin_amdgcn_readlane(x.n, l);
+                    q.base = __builtin_amdgcn_readlane(x.base, l);
+                    q.len = __builtin_amdgcn_readlane(x.len, l);
+                    q.row_tiles = __builtin_amdgcn_readlane(x.row_tiles, l);
+                    q.most = __builtin_amdgcn_readlane(x.most, l);
+                    first = __builtin_amdgcn_readlane(sum - n, l);
+                    s.b = c + l;
+                    found = true;
+                    break;
+                }
+                before = __builtin_amdgcn_readlane(sum, 63);
+            }
+            if (!found) return false;
+        }
+        cuts = max((q.most + step - 1) / step, 1u);
+    }
+    s.split = 0;
+    if (item >= 0) {  // (the last rows have the most keys: first)
+        const int nth = cuts == 1 ? item - first : static_cast<int>(static_cast<uint32_t>(item - first) / static_cast<uint32_t>(cuts));
+        s.rt = q.row_tiles - 1 - nth;
+        s.split = item - first - nth * cuts;
+    }
+    if (s.rt < 0 || s.rt >= q.row_tiles) return false;
+    s.row0 = q.row0;
+    s.base = q.base;
+    s.len = q.len;
+    s.n_rows = q.n * p.R;
+    s.item0 = first + static_cast<int64_t>(q.row_tiles - 1 - s.rt) * cuts;
+    s.lo = q.base + p.by_R.of(s.rt * rows);
+    s.hi = q.base + p.by_R.of(min((s.rt + 1) * rows, s.n_rows) - 1);
+    s.span = kv_span<TOK>(a, p, s.lo, s.hi, q.len);
     s.share = s.span.tiles;
     s.live = 1;
-    if (p.splits > 1) {
-        const int last = (s.n_rows - 1) / rows * rows;
-        const int most = kv_span<TOK>(a, p, s.base + p.by_R.of(last), s.base + n - 1, s.len).tiles;
-        s.share = max(p.by_splits.of(most + p.splits - 1), p.min_tiles);
-        s.live = 1;
-        for (int at = s.share; at < s.span.tiles; at += s.share) ++s.live;
+    if (cuts > 1) {
+        s.share = max(static_cast<int>(static_cast<uint32_t>(q.most + cuts - 1) / static_cast<uint32_t>(cuts)), p.min_tiles);
+        s.live = max(static_cast<int>(static_cast<uint32_t>(s.span.tiles + s.share - 1) / static_cast<uint32_t>(s.share)), 1);
     }
-    return true;
+    return s.split < s.live && s.item0 + s.split < p.items;
 }
 
 // Over lanes l, l ^ 16, l ^ 32, l ^ 48, in all of them (the swaps leave the rows of 16 and the halves beside each other).
@@ -137,9 +257,10 @@ __global__ __launch_bounds__(256, D * NR <= 128 && NG <= 2 ? 3 : 2) void k_kv_at
     const CodePair code_pair;
     const uint32_t ln = threadIdx.x & 63u, m = ln & 15u, g = ln >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int rt = p.by_splits.of(blockIdx.x), split = blockIdx.x - rt * p.splits, h = blockIdx.y, b = blockIdx.z;
     KvShare w;
-    if (!kv_share<kKvTile>(a, p, b, rt, ROWS, w) || split >= w.live) return;
+    const int item = p.by_heads.of(blockIdx.x), h = blockIdx.x - item * a.heads;
+    if (!kv_share<kKvTile>(a, p, ROWS, item, w)) return;
+    const int rt = w.rt, split = w.split, b = w.b;
     const int64_t row0 = w.row0;
     const int n_rows = w.n_rows, base = w.base, len = w.len, lo = w.lo, hi = w.hi, live = w.live, share = w.share;
     const KvSpan span = w.span;
@@ -447,7 +568,7 @@ __global__ __launch_bounds__(256, D * NR <= 128 && NG <= 2 ? 3 : 2) void k_kv_at
             for (int t = 0; t < NT; ++t)
                 *reinterpret_cast<uint2 *>(dst + 32 * t) = make_uint2(pack_bf16x2(o[r][t][0] * inv, o[r][t][1] * inv), pack_bf16x2(o[r][t][2] * inv, o[r][t][3] * inv));
         } else {
-            const int64_t at = (((static_cast<int64_t>(b) * a.heads + h) * p.row_tiles + rt) * p.splits + split) * ROWS + 16 * r + m;
+            const int64_t at = (h * static_cast<int64_t>(p.items) + w.item0 + split) * ROWS + 16 * r + m;
             float *dst = p.part + at * D + 4 * g;
 #pragma unroll
             for (int t = 0; t < NT; ++t) *reinterpret_cast<f32x4 *>(dst + 16 * t) = o[r][t];
@@ -490,10 +611,10 @@ __global__ __launch_bounds__(64 * W, D == 256 ? 1 : 2) void k_kv_attend_many(KvA
     __shared__ uint32_t reduced[3];
     const uint32_t ln = threadIdx.x & 63u, c32 = ln & 31u, hh = ln >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int tile_id = p.by_splits.of(blockIdx.x), split = blockIdx.x - tile_id * p.splits, h = blockIdx.y, b = blockIdx.z;
-    const int rt = p.row_tiles - 1 - tile_id;  // (the last rows have the most keys: first)
     KvShare w;
-    if (!kv_share<TOK>(a, p, b, rt, ROWS, w) || split >= w.live) return;
+    const int item = p.by_heads.of(blockIdx.x), h = blockIdx.x - item * a.heads;
+    if (!kv_share<TOK>(a, p, ROWS, item, w)) return;
+    const int rt = w.rt, split = w.split, b = w.b;
     const int v0 = split * w.share, v1 = min(v0 + w.share, w.span.tiles);
     const int wrow = rt * ROWS + 32 * wave;
     const int wlo = w.base + p.by_R.of(wrow);  // the wave's first and last position
@@ -955,7 +1076,7 @@ __global__ __launch_bounds__(64 * W, D == 256 ? 1 : 2) void k_kv_attend_many(KvA
                 *reinterpret_cast<uint2 *>(dst + 64 * t + 4 * e) =
                     make_uint2(pack_bf16x2(o[t][e] * inv, o[t][e + 1] * inv), pack_bf16x2(o[t][e + 2] * inv, o[t][e + 3] * inv));
     } else {
-        const int64_t at = (((static_cast<int64_t>(b) * a.heads + h) * p.row_tiles + rt) * p.splits + split) * ROWS + (row - rt * ROWS);
+        const int64_t at = (h * static_cast<int64_t>(p.items) + w.item0 + split) * ROWS + (row - rt * ROWS);
         float *dst = p.part + at * D + 4 * hh;
         const float f = v_undo;
 #pragma unroll
@@ -973,11 +1094,12 @@ template <int D, int TOK>
 __global__ __launch_bounds__(256) void k_kv_join(KvArgs a, KvAttendArgs p, int rows)
 {
     constexpr int LPR = D / 4, RPW = 256 / LPR;
-    const int h = blockIdx.y, b = blockIdx.z, c = threadIdx.x % LPR;
-    const int row = blockIdx.x * RPW + threadIdx.x / LPR, rt = row / rows;
+    const int h = blockIdx.y, c = threadIdx.x % LPR, row = blockIdx.x * RPW + threadIdx.x / LPR;
     KvShare w;
-    if (!kv_share<TOK>(a, p, b, rt, rows, w) || row >= w.n_rows || w.live == 1) return;
-    const int64_t at = (((static_cast<int64_t>(b) * a.heads + h) * p.row_tiles + rt) * p.splits) * rows + (row - rt * rows);
+    w.b = blockIdx.z;
+    w.rt = p.by_rows.of(blockIdx.x * RPW);  // (a tile's rows are a multiple of RPW)
+    if (!kv_share<TOK>(a, p, rows, -1, w) || row >= w.n_rows || w.live == 1 || w.item0 + w.live > p.items) return;
+    const int64_t at = (h * static_cast<int64_t>(p.items) + w.item0) * rows + (row - w.rt * rows);
     const float *part = p.part + at * D + 4 * c;
     const float2 *ml = reinterpret_cast<const float2 *>(p.part_ml) + at;
     float mx = kKvLowest, l = 0.0f;
@@ -1016,41 +1138,58 @@ __global__ __launch_bounds__(256) void k_kv_join(KvArgs a, KvAttendArgs p, int r
 struct KvChoice {
     bool many;
     int rows, row_tiles, splits, min_tiles;
+    int64_t items;
+    size_t partial_rows;  // of the workspace, whatever number of rows the tensors have
 };
 
-static KvChoice choose(const KvArgs &a, int D, int R, int max_len, int compute_units)
+static KvChoice choose(const KvArgs &a, int D, int R, int reach, int compute_units)
 {
     KvChoice c;
     const int most = a.max_new * R;  // rows of a head and sequence
+    // The few rows' kernel reads the cache once for 16 of them, or for 32; the other one dequantises every tile, for 128 or 256 (64 rows of which
+    // 32 used: 55 us to 39 at 4096 tokens, 16 sequences, 8 heads of 128; all 64: 58 to 64, with four groups a head 64 to 98).
     c.many = most > 32;
     c.rows = c.many ? 128 : most > 16 && D <= 128 && a.ng == 1 ? 32 : 16;
+    // 256 rows a workgroup dequantise a tile half as often as 128, if they fill the device and are most of a tile (4096 tokens over
+    // 16384, 32 heads: 1060 us and 1110; 2048 over 2048, 5 heads, which do not: 38 and 36).
     if (c.many && D <= 128) {
         const int64_t big = std::min<int64_t>(static_cast<int64_t>(a.n_seqs) * ((most + 255) / 256), a.rows * R / 256 + a.n_seqs);
         if (a.heads * big >= compute_units && a.rows * R >= 512ll * a.n_seqs) c.rows = 256;
     }
-    c.row_tiles = (most + c.rows - 1) / c.rows;
     const int tok = !c.many ? kKvTile : D == 256 ? 32 : 64;
+    // at least 128 tokens a share, a step for each wave, or 256 ones that many rows take together
     c.min_tiles = 128 * (c.many ? 2 : 1) / tok;
-    // workgroups without a split: no more than the rows there are and one more of each sequence
-    const int64_t groups = a.heads * std::min<int64_t>(static_cast<int64_t>(a.n_seqs) * c.row_tiles, a.rows * R / c.rows + a.n_seqs);
-    const int64_t tiles = (max_len + tok - 1) / tok + 1;
-    const int64_t slots = (c.many ? 1 : 3) * compute_units;
-    const int64_t want = slots / std::max<int64_t>(groups, 1);
-    c.splits = static_cast<int>(std::min<int64_t>(std::max<int64_t>(std::min(want, tiles / c.min_tiles), 1), 256));
+    const int64_t slots = std::max<int64_t>((c.many ? 1 : 3) * compute_units / a.heads, 1);
+    const int64_t cuts = std::min<int64_t>(((reach + tok - 1) / tok + 1) / c.min_tiles, 256);
+    // Where tiles of rows fill the device uncut, a long sequence among short ones is cut all the same, if there may be one (one
+    // of 100 000 tokens among 99 of 200 to 1000, 8 heads: 69 us, uncut 953; 64 equal ones of 8192, 40 heads: 344 and 346).
+    const bool always = !c.many && reach >= 8192;
+    const auto tiles_of = [&](int rows) { return static_cast<int64_t>((most + rows - 1) / rows); };
+    const auto listed = [&](int64_t groups) { return std::min(std::max(slots, groups + std::max<int64_t>(groups / 2, 1)), groups * cuts); };
+    c.row_tiles = tiles_of(c.rows);
+    // tiles of rows: no more than the rows there are and one more of each sequence
+    const int64_t all = a.n_seqs * tiles_of(c.rows), groups = std::min(all, a.rows * R / c.rows + a.n_seqs);
+    c.splits = 1;
+    c.items = groups;
+    if (cuts > 1 && (slots > groups || (always && a.n_seqs > 1))) {
+        c.splits = a.n_seqs > 1 ? 2 : std::max<int64_t>(std::min(slots / groups, cuts), 1);
+        c.items = a.n_seqs > 1 ? listed(groups) : groups * c.splits;
+    }
+    // (fewer rows than sequences times max_new may leave room for shares; tiles of 256 rows fill the device uncut)
+    c.partial_rows = 0;
+    if (cuts > 1) {
+        const int rows = c.many ? 128 : c.rows;
+        const int64_t top = std::min(a.n_seqs * tiles_of(rows), always ? INT64_MAX : slots - 1);
+        if (top > 0) c.partial_rows = static_cast<size_t>(a.heads) * rows * std::max(listed(top), std::min(slots, top * cuts));
+    }
     return c;
-}
-
-static size_t partial_rows(const KvArgs &a, const KvChoice &c)
-{
-    return static_cast<size_t>(a.n_seqs) * a.heads * c.row_tiles * c.splits * c.rows;
 }
 
 size_t kv_attend_workspace_bytes(const KvArgs &a, int D, int R, int max_len)
 {
     int cu;
     if (compute_units_of_current_device(&cu) != hipSuccess) return 0;
-    const KvChoice c = choose(a, D, R, max_len, cu);
-    return c.splits == 1 ? 16 : partial_rows(a, c) * (D + 2) * sizeof(float);
+    return std::max<size_t>(choose(a, D, R, max_len, cu).partial_rows * (D + 2) * sizeof(float), 16);
 }
 
 template <int D>
@@ -1098,7 +1237,7 @@ template <int D, int TOK>
 static void launch_join(const KvArgs &a, const KvAttendArgs &p, const KvChoice &c, hipStream_t s)
 {
     constexpr int per = 256 / (D / 4);
-    const dim3 grid((a.max_new * p.R + per - 1) / per, a.heads, a.n_seqs);
+    const dim3 grid((std::min<int64_t>(a.max_new, a.rows) * p.R + per - 1) / per, a.heads, a.n_seqs);
     if (c.many) hipLaunchKernelGGL((k_kv_join<D, TOK>), grid, dim3(256), 0, s, a, p, c.rows);
     else hipLaunchKernelGGL((k_kv_join<D, kKvTile>), grid, dim3(256), 0, s, a, p, c.rows);
 }
@@ -1108,15 +1247,21 @@ int launch_kv_attend(const KvArgs &a, KvAttendArgs p, int D, int max_len, void *
     int cu;
     hipError_t e = compute_units_of_current_device(&cu);
     if (e != hipSuccess) return hip_result(e);
-    const KvChoice c = choose(a, D, p.R, max_len, cu);
+    // tokens that a tile of rows may go through: no more than the workspace was sized for
+    const int64_t reach = p.window == 0 ? max_len : std::min<int64_t>(max_len, static_cast<int64_t>(p.window) + p.sinks + a.max_new);
+    const KvChoice c = choose(a, D, p.R, static_cast<int>(reach), cu);
     p.splits = c.splits;
     p.by_R = KvDivisor(p.R);
     p.by_splits = KvDivisor(c.splits);
+    p.by_heads = KvDivisor(a.heads);
+    p.by_rows = KvDivisor(c.rows);
+    p.items = c.items;
     p.row_tiles = c.row_tiles;
     p.min_tiles = c.min_tiles;
     p.part = static_cast<float *>(workspace);
-    p.part_ml = p.part + partial_rows(a, c) * D;
-    const dim3 grid(static_cast<uint32_t>(c.splits) * c.row_tiles, a.heads, a.n_seqs);
+    p.part_ml = p.part + static_cast<size_t>(a.heads) * c.items * c.rows * D;
+    if (c.items * a.heads > kKvMaxItems) return TPQ_ERR_SHAPE;
+    const dim3 grid(static_cast<uint32_t>(c.items) * a.heads);
     if (c.many) {
         e = D == 256 ? launch_many_of<256, 4, 32>(a, p, grid, s)
             : c.rows == 256 ? (D == 64 ? launch_many_of<64, 8, 64>(a, p, grid, s) : launch_many_of<128, 8, 64>(a, p, grid, s))
