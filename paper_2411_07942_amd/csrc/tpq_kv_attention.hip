@@ -60,18 +60,7 @@ __device__ __forceinline__ KvSeq kv_seq(const KvArgs &a, const KvAttendArgs &p, 
     return q;
 }
 
-// Inclusive sums along the 64 lanes: within rows of 16, then the rows' totals handed on.
-__device__ __forceinline__ uint32_t wave_scan(uint32_t v)
-{
-    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);
-    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
-    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
-    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
-    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);
-    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);
-    return v;
-}
-__device__ __forceinline__ uint32_t wave_total(uint32_t v) { return __builtin_amdgcn_readlane(wave_scan(v), 63); }
+__device__ __forceinline__ uint32_t wave_total(uint32_t v) { return __builtin_amdgcn_readlane(wave_inclusive_sum(v), 63); }
 
 // A workgroup's item: a tile of a sequence's rows and a share of the steps that they go through.  A head's items lie in one
 // list, sequence by sequence and tile by tile, so that no workgroup is without work: one that finds none still costs 11 ns of
@@ -147,7 +136,7 @@ __device__ __forceinline__ bool kv_share(const KvArgs &a, const KvAttendArgs &p,
             uint32_t before = 0;
             for (int c = 0; c < a.n_seqs; c += 64) {
                 const KvSeq x = at(c);
-                const uint32_t n = items_of(x), sum = wave_scan(n) + before;
+                const uint32_t n = items_of(x), sum = wave_inclusive_sum(n) + before;
                 const uint64_t past = __builtin_amdgcn_ballot_w64(static_cast<uint32_t>(item) < sum);
                 if (past) {
                     const int l = __builtin_ctzll(past);
@@ -237,21 +226,33 @@ struct CodePair {
     __device__ __forceinline__ uint32_t operator()(uint32_t w) const { return (w & mask) | base; }
 };
 
+// The value that lane N of the caller's group of RW lanes holds (RW = 2: lane N % 2).
+template <int RW, int N>
+__device__ __forceinline__ float of_group(float v)
+{
+    constexpr int s = RW == 2 ? (N & 1) * 0x55 + 0xA0 : N * 0x55;
+    return dpp_f32<s>(v);
+}
+
 // What a wave reads of a step's 32 tokens: lane (m, g) = (l % 16, l / 16).
-template <int D, int NG>
+template <int D, int NG, bool COLS>
 struct KvRaw {
     static constexpr int KW = D / 32, VW = D == 256 ? 2 : 1;  // words: of a token's quarter of K codes; of a token's chunk of V codes
     uint32_t k[2][KW];       // tokens 16 j + m
     uint32_t v[2][4][VW];    // tokens 16 j + 4 g + i
-    uint32_t meta[NG];       // lane 8 kv + 4 j + i of a row of 16: keys' (kv = 0) or values' scale and zero of token 16 j + 4 g + i
+    static constexpr int X = NG == 8 ? 2 : 1, META = COLS ? 4 * X : NG;
+    uint32_t meta[META];     // COLS: 4 kv + 2 j ... of the lane's group; else lane 8 kv + 4 j + i of a row of 16: keys' (kv = 0) or values' scale and zero of token 16 j + 4 g + i
     bool bad[2];             // (uniform) a page that is none
 };
 
-template <int D, int NG, int NR>
-__global__ __launch_bounds__(256, D * NR <= 128 && NG <= 2 ? 3 : 2) void k_kv_attend_few(KvArgs a, KvAttendArgs p)
+template <int D, int GROUPS, int NR, bool COLS>
+__global__ __launch_bounds__(256, D * NR <= 128 && (COLS || GROUPS <= 2) ? 3 : 2) void k_kv_attend_few(KvArgs a, KvAttendArgs p)
 {
-    constexpr int KK = D / 32, NT = D / 16, KPG = KK / NG, TPG = NT / NG, ROWS = 16 * NR;
-    typedef KvRaw<D, NG> Raw;
+    constexpr int NG = COLS ? 1 : GROUPS;  // groups one after the other
+    constexpr int KK = D / 32, NT = D / 16, KPG = KK / NG, TPG = NT / NG, ROWS = COLS ? 16 / GROUPS : 16 * NR;
+    constexpr int RW = COLS ? 16 / GROUPS : 16;  // columns of a group
+    typedef KvRaw<D, GROUPS, COLS> Raw;
+    static_assert(!COLS || NR == 1, "rows");
     __shared__ float sO[2][ROWS][D + 4];
     __shared__ float sM[2][ROWS], sL[2][ROWS];
     const CodePair code_pair;
@@ -266,13 +267,14 @@ __global__ __launch_bounds__(256, D * NR <= 128 && NG <= 2 ? 3 : 2) void k_kv_at
     const KvSpan span = w.span;
     const int v1 = min((split + 1) * share, span.tiles);
 
-    // queries: column m of the products' right operand
+    // queries: column m of the products' right operand; COLS: column RW gr + r has row r's features of group gr
+    const uint32_t mr = m % RW, mg = m / RW;
     bf16x8_t q[NR][KK];
     float qs[NR][NG];
     int pos[NR];
 #pragma unroll
     for (int r = 0; r < NR; ++r) {
-        const int row = rt * ROWS + 16 * r + static_cast<int>(m);
+        const int row = rt * ROWS + 16 * r + static_cast<int>(mr);
         const int rc = min(row, n_rows - 1), i = p.by_R.of(rc);
         pos[r] = base + i;
         const uint8_t *src = p.Q + (row0 + i) * p.ldQ + (h * p.R + rc - i * p.R) * (2 * D) + 16 * g;
@@ -283,6 +285,7 @@ __global__ __launch_bounds__(256, D * NR <= 128 && NG <= 2 ? 3 : 2) void k_kv_at
             for (int kk = gr * KPG; kk < (gr + 1) * KPG; ++kk) {
                 u32x4 w = *reinterpret_cast<const u32x4 *>(src + 64 * kk);
                 if (p.scale < 0.0f) w ^= 0x80008000u;  // (scores are then multiplied by |scale|: their order is the products')
+                if (COLS && static_cast<uint32_t>(kk * GROUPS / KK) != mg) w = u32x4{0, 0, 0, 0};
                 q[r][kk] = __builtin_bit_cast(bf16x8_t, w);
                 const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
@@ -323,9 +326,21 @@ __global__ __launch_bounds__(256, D * NR <= 128 && NG <= 2 ? 3 : 2) void k_kv_at
                 for (int w = 0; w < Raw::VW; ++w) raw.v[j][i][w] = reinterpret_cast<const uint32_t *>(vc + vo + i * (D / 2))[w];
             metas[j] = cell + page_len * D + 4 * slot;
         }
-        const uint8_t *meta = (m & 4u ? metas[1] : metas[0]) + (m & 8u ? 4 * NG * page_len : 0u) + 16 * g + 4 * (m & 3u);
+        if constexpr (COLS) {
+            // a lane's own group's, token 4 g + m % 4 (RW = 2: 4 g + 2 x + m % 2)
+            const uint32_t at = mg * page_len + 4 * g + (m & (RW == 2 ? 1u : 3u));
 #pragma unroll
-        for (int gr = 0; gr < NG; ++gr) raw.meta[gr] = *reinterpret_cast<const uint32_t *>(meta + 4 * (gr * page_len));
+            for (int kv = 0; kv < 2; ++kv)
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+#pragma unroll
+                    for (int x = 0; x < Raw::X; ++x)
+                        raw.meta[(2 * kv + j) * Raw::X + x] = *reinterpret_cast<const uint32_t *>(metas[j] + 4 * (at + kv * GROUPS * page_len + 2 * x));
+        } else {
+            const uint8_t *meta = (m & 4u ? metas[1] : metas[0]) + (m & 8u ? 4 * NG * page_len : 0u) + 16 * g + 4 * (m & 3u);
+#pragma unroll
+            for (int gr = 0; gr < NG; ++gr) raw.meta[gr] = *reinterpret_cast<const uint32_t *>(meta + 4 * (gr * page_len));
+        }
     };
 
     f32x4 o[NR][NT], oc[NR];  // accumulators; row gr of oc: 128 * (sum of group gr's weights as the products see them)
@@ -346,6 +361,24 @@ __global__ __launch_bounds__(256, D * NR <= 128 && NG <= 2 ? 3 : 2) void k_kv_at
     const int window = p.window > 0 ? p.window : 1 << 30;
     const float k_score = p.softcap > 0.0f ? 1.0f : fabsf(p.scale) * log2e;
     const float cap_in = p.softcap > 0.0f ? fabsf(p.scale) / p.softcap * 2.0f * log2e : 0.0f, cap_out = p.softcap * log2e;
+
+    // scale or zero of key (kv = 0) or value 16 J + 4 g + I, for the caller's group
+    auto meta_of = [&](auto kv, auto jj, auto ii, const float (&from)[Raw::META], int gr) __attribute__((always_inline)) {
+        constexpr int KV = decltype(kv)::value, J = decltype(jj)::value, I = decltype(ii)::value;
+        if constexpr (COLS) return of_group<RW, I>(from[(2 * KV + J) * Raw::X + (Raw::X == 2 ? I / 2 : 0)]);
+        else return of_row<8 * KV + 4 * J + I>(from[gr]);
+    };
+    constexpr std::integral_constant<int, 0> of_keys{};
+    constexpr std::integral_constant<int, 1> of_values{};
+
+    auto metas_of = [&](const Raw &raw, int gr, float (&sc)[Raw::META], float (&ze)[Raw::META]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int x = 0; x < Raw::META; ++x)
+            if (COLS || x == gr) {
+                sc[x] = bf16_lo_to_f32(raw.meta[x]);
+                ze[x] = bf16_hi_to_f32(raw.meta[x]);
+            }
+    };
 
     auto step = [&](const Raw &raw, int v) {
         const int t0 = span.tile(v) * kKvTile;
@@ -371,14 +404,19 @@ __global__ __launch_bounds__(256, D * NR <= 128 && NG <= 2 ? 3 : 2) void k_kv_at
                     for (int r = 0; r < NR; ++r)
                         acc[r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, c), q[r][kk], acc[r], 0, 0, 0);
                 }
-                const float sc = bf16_lo_to_f32(raw.meta[gr]), ze = bf16_hi_to_f32(raw.meta[gr]);
+                float sc[Raw::META], ze[Raw::META];
+                metas_of(raw, gr, sc, ze);
                 for_each<4>([&](auto i) {
                     constexpr int I = decltype(i)::value;
                     // (products, whose operand the exchange goes into; multiply-adds would take a move for each)
 #pragma unroll
                     for (int r = 0; r < NR; ++r) {
-                        const float x = of_row<4 * J + I>(sc) * acc[r][I], z = of_row<4 * J + I>(ze) * qs[r][gr];
+                        const float x = meta_of(of_keys, jj, i, sc, gr) * acc[r][I], z = meta_of(of_keys, jj, i, ze, gr) * qs[r][gr];
                         s[r][J][I] = gr == 0 ? x + z : (s[r][J][I] + x) + z;
+                        // the groups' parts (in an order that leaves the same sum in all of them)
+                        if (COLS && RW <= 8) s[r][J][I] += dpp_f32<0x128>(s[r][J][I]);
+                        if (COLS && RW <= 4) s[r][J][I] += dpp_f32<0x124>(s[r][J][I]);
+                        if (COLS && RW <= 2) s[r][J][I] += dpp_f32<0x122>(s[r][J][I]);
                     }
                 });
             }
@@ -428,7 +466,8 @@ __global__ __launch_bounds__(256, D * NR <= 128 && NG <= 2 ? 3 : 2) void k_kv_at
 #pragma unroll
         for (int gr = 0; gr < NG; ++gr) {
             bf16x8_t bh[NR], bl[NR];
-            const float sc = bf16_lo_to_f32(raw.meta[gr]), ze = bf16_hi_to_f32(raw.meta[gr]);
+            float sc[Raw::META], ze[Raw::META];
+            metas_of(raw, gr, sc, ze);
 #pragma unroll
             for (int r = 0; r < NR; ++r) {
                 u32x4 ph, pl;
@@ -437,17 +476,17 @@ __global__ __launch_bounds__(256, D * NR <= 128 && NG <= 2 ? 3 : 2) void k_kv_at
                     float w[4];
                     for_each<4>([&](auto i) {
                         constexpr int I = decltype(i)::value;
-                        w[I] = of_row<8 + 4 * J + I>(sc) * s[r][J][I];
+                        w[I] = meta_of(of_values, jj, i, sc, gr) * s[r][J][I];
                     });
                     if (whole) {
                         for_each<4>([&](auto i) {
                             constexpr int I = decltype(i)::value;
-                            zs[r][gr] += of_row<8 + 4 * J + I>(ze) * s[r][J][I];
+                            zs[r][gr] += meta_of(of_values, jj, i, ze, gr) * s[r][J][I];
                         });
                     } else {  // (what lies behind a hidden key may be anything)
                         for_each<4>([&](auto i) {
                             constexpr int I = decltype(i)::value;
-                            const float z = of_row<8 + 4 * J + I>(ze) * s[r][J][I];
+                            const float z = meta_of(of_values, jj, i, ze, gr) * s[r][J][I];
                             zs[r][gr] += vis[r][J][I] ? z : 0.0f;
                             w[I] = vis[r][J][I] ? w[I] : 0.0f;
                         });
@@ -527,6 +566,8 @@ __global__ __launch_bounds__(256, D * NR <= 128 && NG <= 2 ? 3 : 2) void k_kv_at
             for (int t = gr * TPG; t < (gr + 1) * TPG; ++t) o[r][t] = o[r][t] - c + z;
         }
     }
+    // (COLS: a lane's accumulators are its column's, of which those of its own group count)
+    const auto mine = [&](int t) { return !COLS || static_cast<uint32_t>(t * GROUPS / NT) == mg; };
     // the four waves' results into wave 0's: 2 and 3 to 0 and 1, then 1 to 0
 #pragma unroll
     for (int from = 2; from >= 1; from >>= 1) {
@@ -534,10 +575,11 @@ __global__ __launch_bounds__(256, D * NR <= 128 && NG <= 2 ? 3 : 2) void k_kv_at
 #pragma unroll
             for (int r = 0; r < NR; ++r) {
 #pragma unroll
-                for (int t = 0; t < NT; ++t) *reinterpret_cast<f32x4 *>(&sO[wave - from][16 * r + m][16 * t + 4 * g]) = o[r][t];
-                if (g == 0) {
-                    sM[wave - from][16 * r + m] = mx[r];
-                    sL[wave - from][16 * r + m] = l[r];
+                for (int t = 0; t < NT; ++t)
+                    if (mine(t)) *reinterpret_cast<f32x4 *>(&sO[wave - from][16 * r + mr][16 * t + 4 * g]) = o[r][t];
+                if (g == 0 && mg == 0) {
+                    sM[wave - from][16 * r + mr] = mx[r];
+                    sL[wave - from][16 * r + mr] = l[r];
                 }
             }
         }
@@ -545,12 +587,13 @@ __global__ __launch_bounds__(256, D * NR <= 128 && NG <= 2 ? 3 : 2) void k_kv_at
         if (wave < from) {
 #pragma unroll
             for (int r = 0; r < NR; ++r) {
-                const float m2 = sM[wave][16 * r + m], now = fmaxf(mx[r], m2);
+                const float m2 = sM[wave][16 * r + mr], now = fmaxf(mx[r], m2);
                 const float f1 = __builtin_amdgcn_exp2f(mx[r] - now), f2 = __builtin_amdgcn_exp2f(m2 - now);
                 mx[r] = now;
-                l[r] = l[r] * f1 + sL[wave][16 * r + m] * f2;
+                l[r] = l[r] * f1 + sL[wave][16 * r + mr] * f2;
 #pragma unroll
-                for (int t = 0; t < NT; ++t) o[r][t] = o[r][t] * f1 + *reinterpret_cast<const f32x4 *>(&sO[wave][16 * r + m][16 * t + 4 * g]) * f2;
+                for (int t = 0; t < NT; ++t)
+                    if (mine(t)) o[r][t] = o[r][t] * f1 + *reinterpret_cast<const f32x4 *>(&sO[wave][16 * r + mr][16 * t + 4 * g]) * f2;
             }
         }
         __syncthreads();
@@ -558,7 +601,7 @@ __global__ __launch_bounds__(256, D * NR <= 128 && NG <= 2 ? 3 : 2) void k_kv_at
     if (wave != 0) return;
 #pragma unroll
     for (int r = 0; r < NR; ++r) {
-        const int row = rt * ROWS + 16 * r + static_cast<int>(m);
+        const int row = rt * ROWS + 16 * r + static_cast<int>(mr);
         if (row >= n_rows) continue;
         if (live == 1) {
             const int i = p.by_R.of(row);
@@ -566,13 +609,14 @@ __global__ __launch_bounds__(256, D * NR <= 128 && NG <= 2 ? 3 : 2) void k_kv_at
             const float inv = l[r] > 0.0f ? 1.0f / l[r] : 0.0f;
 #pragma unroll
             for (int t = 0; t < NT; ++t)
-                *reinterpret_cast<uint2 *>(dst + 32 * t) = make_uint2(pack_bf16x2(o[r][t][0] * inv, o[r][t][1] * inv), pack_bf16x2(o[r][t][2] * inv, o[r][t][3] * inv));
+                if (mine(t)) *reinterpret_cast<uint2 *>(dst + 32 * t) = make_uint2(pack_bf16x2(o[r][t][0] * inv, o[r][t][1] * inv), pack_bf16x2(o[r][t][2] * inv, o[r][t][3] * inv));
         } else {
-            const int64_t at = (h * static_cast<int64_t>(p.items) + w.item0 + split) * ROWS + 16 * r + m;
+            const int64_t at = (h * static_cast<int64_t>(p.items) + w.item0 + split) * ROWS + 16 * r + mr;
             float *dst = p.part + at * D + 4 * g;
 #pragma unroll
-            for (int t = 0; t < NT; ++t) *reinterpret_cast<f32x4 *>(dst + 16 * t) = o[r][t];
-            if (g == 0) *reinterpret_cast<float2 *>(p.part_ml + 2 * at) = make_float2(mx[r], l[r]);
+            for (int t = 0; t < NT; ++t)
+                if (mine(t)) *reinterpret_cast<f32x4 *>(dst + 16 * t) = o[r][t];
+            if (g == 0 && mg == 0) *reinterpret_cast<float2 *>(p.part_ml + 2 * at) = make_float2(mx[r], l[r]);
         }
     }
 }
@@ -1136,7 +1180,7 @@ __global__ __launch_bounds__(256) void k_kv_join(KvArgs a, KvAttendArgs p, int r
 // ---- host -----------------------------------------------------------------------------------
 
 struct KvChoice {
-    bool many;
+    bool many, cols;
     int rows, row_tiles, splits, min_tiles;
     int64_t items;
     size_t partial_rows;  // of the workspace, whatever number of rows the tensors have
@@ -1149,7 +1193,8 @@ static KvChoice choose(const KvArgs &a, int D, int R, int reach, int compute_uni
     // The few rows' kernel reads the cache once for 16 of them, or for 32; the other one dequantises every tile, for 128 or 256 (64 rows of which
     // 32 used: 55 us to 39 at 4096 tokens, 16 sequences, 8 heads of 128; all 64: 58 to 64, with four groups a head 64 to 98).
     c.many = most > 32;
-    c.rows = c.many ? 128 : most > 16 && D <= 128 && a.ng == 1 ? 32 : 16;
+    c.cols = a.ng > 1 && most * a.ng <= 16;
+    c.rows = c.many ? 128 : c.cols ? 16 / a.ng : most > 16 && D <= 128 && a.ng == 1 ? 32 : 16;
     // 256 rows a workgroup dequantise a tile half as often as 128, if they fill the device and are most of a tile (4096 tokens over
     // 16384, 32 heads: 1060 us and 1110; 2048 over 2048, 5 heads, which do not: 38 and 36).
     if (c.many && D <= 128) {
@@ -1193,13 +1238,13 @@ size_t kv_attend_workspace_bytes(const KvArgs &a, int D, int R, int max_len)
 }
 
 template <int D>
-static auto few_kernel(int ng)
+static auto few_kernel(int ng, bool cols)
 {
     switch (ng) {
-    case 1: return k_kv_attend_few<D, 1, 1>;
-    case 2: return k_kv_attend_few<D, 2, 1>;
-    case 4: return k_kv_attend_few<D, D >= 128 ? 4 : 2, 1>;
-    default: return k_kv_attend_few<D, D >= 256 ? 8 : 2, 1>;
+    case 1: return k_kv_attend_few<D, 1, 1, false>;
+    case 2: return cols ? k_kv_attend_few<D, 2, 1, true> : k_kv_attend_few<D, 2, 1, false>;
+    case 4: return cols ? k_kv_attend_few<D, D >= 128 ? 4 : 2, 1, true> : k_kv_attend_few<D, D >= 128 ? 4 : 2, 1, false>;
+    default: return cols ? k_kv_attend_few<D, D >= 256 ? 8 : 2, 1, true> : k_kv_attend_few<D, D >= 256 ? 8 : 2, 1, false>;
     }
 }
 
@@ -1268,9 +1313,9 @@ int launch_kv_attend(const KvArgs &a, KvAttendArgs p, int D, int max_len, void *
                             : (D == 64 ? launch_many_of<64, 4, 64>(a, p, grid, s) : launch_many_of<128, 4, 64>(a, p, grid, s));
         if (e != hipSuccess) return hip_result(e);
     } else {
-        const auto kernel = D == 256 ? few_kernel<256>(a.ng)
-                            : c.rows == 32 ? (D == 64 ? k_kv_attend_few<64, 1, 2> : k_kv_attend_few<128, 1, 2>)
-                                           : (D == 64 ? few_kernel<64>(a.ng) : few_kernel<128>(a.ng));
+        const auto kernel = D == 256 ? few_kernel<256>(a.ng, c.cols)
+                            : c.rows == 32 ? (D == 64 ? k_kv_attend_few<64, 1, 2, false> : k_kv_attend_few<128, 1, 2, false>)
+                                           : (D == 64 ? few_kernel<64>(a.ng, c.cols) : few_kernel<128>(a.ng, c.cols));
         launch_kernel(kernel, grid, dim3(256), 0, s, a, p);
     }
     if (c.splits > 1) {
