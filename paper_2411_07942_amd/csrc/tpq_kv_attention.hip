@@ -1141,7 +1141,7 @@ __global__ __launch_bounds__(256) void k_kv_join(KvArgs a, KvAttendArgs p, int r
     const int h = blockIdx.y, c = threadIdx.x % LPR, row = blockIdx.x * RPW + threadIdx.x / LPR;
     KvShare w;
     w.b = blockIdx.z;
-    w.rt = p.by_rows.of(blockIdx.x * RPW);  // (a tile's rows are a multiple of RPW)
+    w.rt = p.by_rows.of(row);
     if (!kv_share<TOK>(a, p, rows, -1, w) || row >= w.n_rows || w.live == 1 || w.item0 + w.live > p.items) return;
     const int64_t at = (h * static_cast<int64_t>(p.items) + w.item0) * rows + (row - w.rt * rows);
     const float *part = p.part + at * D + 4 * c;
@@ -1190,10 +1190,14 @@ static KvChoice choose(const KvArgs &a, int D, int R, int reach, int compute_uni
 {
     KvChoice c;
     const int most = a.max_new * R;  // rows of a head and sequence
-    // The few rows' kernel reads the cache once for 16 of them, or for 32; the other one dequantises every tile, for 128 or 256 (64 rows of which
-    // 32 used: 55 us to 39 at 4096 tokens, 16 sequences, 8 heads of 128; all 64: 58 to 64, with four groups a head 64 to 98).
-    c.many = most > 32;
-    c.cols = a.ng > 1 && most * a.ng <= 16;
+    // The few rows' kernel reads the cache once for 16 of them, or for 32; the other one dequantises every tile, for 128 or 256 (16
+    // sequences of 4096 tokens, 8 heads of 128: 32 rows 39 us to the other's 55, 64 rows 64 to 58; 4 groups 52 to 63, 98 to 64).
+    // Of 8 groups it takes two rows at once (heads of 256: 4 rows 72 us to 135, 8 rows 118 to 136, 16 rows 214 to 136).
+    c.many = most > (a.ng == 8 ? 8 : 32);
+    // A column for each row and group: one accumulation for all groups, but only 16 / ng rows a tile.  Two tiles of it are still
+    // faster than one of 16 rows whose groups come one after the other if those are 4 (8 rows of heads of 128: 35 us to 40, 16 rows 62
+    // to 42), not if they are 2 (16 rows 35 to 28); with heads of 256 and 4 groups the latter lacks registers (16 rows 91 to 151).
+    c.cols = a.ng > 1 && !c.many && (a.ng == 8 || (D == 256 && a.ng == 4) || most * a.ng <= (a.ng == 4 ? 32 : 16));
     c.rows = c.many ? 128 : c.cols ? 16 / a.ng : most > 16 && D <= 128 && a.ng == 1 ? 32 : 16;
     // 256 rows a workgroup dequantise a tile half as often as 128, if they fill the device and are most of a tile (4096 tokens over
     // 16384, 32 heads: 1060 us and 1110; 2048 over 2048, 5 heads, which do not: 38 and 36).
@@ -1240,12 +1244,13 @@ size_t kv_attend_workspace_bytes(const KvArgs &a, int D, int R, int max_len)
 template <int D>
 static auto few_kernel(int ng, bool cols)
 {
-    switch (ng) {
-    case 1: return k_kv_attend_few<D, 1, 1, false>;
-    case 2: return cols ? k_kv_attend_few<D, 2, 1, true> : k_kv_attend_few<D, 2, 1, false>;
-    case 4: return cols ? k_kv_attend_few<D, D >= 128 ? 4 : 2, 1, true> : k_kv_attend_few<D, D >= 128 ? 4 : 2, 1, false>;
-    default: return cols ? k_kv_attend_few<D, D >= 256 ? 8 : 2, 1, true> : k_kv_attend_few<D, D >= 256 ? 8 : 2, 1, false>;
+    if constexpr (D == 256) {
+        if (ng == 8) return k_kv_attend_few<D, 8, 1, true>;
+        if (ng == 4) return k_kv_attend_few<D, 4, 1, true>;
     }
+    if constexpr (D == 128)
+        if (ng == 4) return cols ? k_kv_attend_few<D, 4, 1, true> : k_kv_attend_few<D, 4, 1, false>;
+    return ng == 1 ? k_kv_attend_few<D, 1, 1, false> : cols ? k_kv_attend_few<D, 2, 1, true> : k_kv_attend_few<D, 2, 1, false>;
 }
 
 // Two tiles of keys and of values, heads of 256 their queries too: more than the default limit of LDS, allowed once per device.
