@@ -358,11 +358,11 @@ int tpq_decode_reduce_static(const tpq_layout *L, const void *plan, int n_ranks,
  *     max_new  no sequence has more new tokens (those past it are left out)
  *     max_len  a hint: no sequence is expected to be longer (how the work is split goes by it;
  *              a longer sequence costs time only); at most ld_table * page
- *     rows     rows of the batch's matrices; those behind the last sequence are neither read
+ *     rows     rows of the batch's matrices; those behind the last sequence are neither used
  *              nor written
  * Everything on the device may change between calls (and replays of a captured call) within
  * these host numbers.  Nothing outside the buffers is ever touched: a sequence whose starts lie
- * outside 0..rows or decrease is left out, a token whose page number is outside 0..n_pages - 1, or
+ * outside 0..rows or decrease is left out (others of such a batch may be, too), a token whose page number is outside 0..n_pages - 1, or
  * whose position is outside the table, counts as absent: not written, not read, not seen.
  * tpq_kv_check reports all of these. */
 #define TPQ_KV_MAX_HEADS 256

@@ -15,22 +15,6 @@ struct KvArgs {
     uint32_t cell_bytes;
 };
 
-struct KvAppendArgs {
-    const uint8_t *K, *V, *Q;
-    uint8_t *Q_out;
-    int64_t ldK, ldV, ldQ, ldQo;  // bytes
-    const float *cosines, *sines;
-    int32_t rot, rot_rows, pairs;
-    int32_t units;  // head rows of a token: 2 heads + q_heads
-};
-
-struct KvReadArgs {
-    uint8_t *K, *V;
-    int64_t ldK, ldV;  // bytes
-    int32_t fp32;
-    int32_t first, units;  // head rows of a token: [first, first + units) of the keys' and the values' heads
-};
-
 // Division by a number that the host knows: two multiplications' worth of scalar instructions instead of the 40 of an
 // integer division (eight of them took 0.4 us in front of a kernel's first load).
 struct KvDivisor {
@@ -50,6 +34,26 @@ struct KvDivisor {
         const uint32_t u = static_cast<uint32_t>(n), t = __umulhi(u, mul);
         return static_cast<int>((t + ((u - t) >> 1)) >> shift);
     }
+};
+
+struct KvAppendArgs {
+    const uint8_t *K, *V, *Q;
+    uint8_t *Q_out;
+    int64_t ldK, ldV, ldQ, ldQo;  // bytes
+    const float *cosines, *sines;
+    int32_t rot, rot_rows, pairs;
+    int32_t units;    // head rows of a token: 2 heads + q_heads
+    int32_t columns;  // workgroups side by side that they take
+    KvDivisor by_columns;
+};
+
+struct KvReadArgs {
+    uint8_t *K, *V;
+    int64_t ldK, ldV;  // bytes
+    int32_t fp32;
+    int32_t first, units;  // head rows of a token: [first, first + units) of the keys' and the values' heads
+    int32_t columns;
+    KvDivisor by_columns;
 };
 
 struct KvAttendArgs {
