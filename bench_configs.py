@@ -18,6 +18,9 @@ This script adds what a deployment asks next, one JSON line per section:
           kernel, beside decode_reduce followed by two elementwise additions;
   gemm    one device's linear layer at the Llama-2-13B shape with the compression in the GEMM's
           epilogue, beside the library GEMM followed by tpq_encode;
+  kv      one device's attention block of the Llama-2-13B shape (5 of 40 heads) over its 4-bit cache, a prompt of 2048 tokens and a
+          decode step of 64 sequences of 1024 to 4096 tokens: append, attention, the linear layer behind it with the compression in its
+          epilogue, the sum over 8 messages, each alone and together; the decode step also replayed from a graph;
   static  the Llama-2-13B-shaped block in the static symmetric mode (per device and feature steps
           from calibration; only codes and selected features travel): encode of all ranks, of one
           rank, decode_reduce in both accumulate modes.
@@ -362,9 +365,65 @@ def section_gemm(tpq, wl, args):
                     "enc1 = that tpq_encode alone"}
 
 
+def section_kv(tpq, wl, args):
+    w = wl.LLAMA_PREFILL
+    N, E, heads, D, page = w.N, w.E, 5, 128, 64
+    dev = "cuda"
+    L = tpq.layout_init(E, w.k, w.G)
+    plan = tpq.plan_build(L, torch.from_numpy(idx_for(wl, w)).to(dev))
+    KL = tpq.kv_layout_init(heads, D, 128, page)
+    g = torch.Generator(device=dev).manual_seed(wl.seed_for(w, 0, 0, 9))
+
+    def rnd(*shape):
+        return torch.randn(shape, generator=g, device=dev).to(torch.bfloat16)
+    Wp = tpq.gemm_weights(L, plan, rnd(E, heads * D) * 0.02)
+    angle = torch.arange(4096, device=dev, dtype=torch.float64)[:, None] * 10000.0 ** (-torch.arange(64, device=dev, dtype=torch.float64) / 64)
+    cos, sin = angle.cos().float(), angle.sin().float()
+
+    def block(lens, new):
+        B, T = len(lens), sum(new)
+        used = [-(-n // page) for n in lens]
+        order = torch.randperm(sum(used), generator=g, device=dev, dtype=torch.int32)
+        table, at = torch.zeros((B, max(used)), dtype=torch.int32, device=dev), 0
+        for b, u in enumerate(used):
+            table[b, :u] = order[at:at + u]
+            at += u
+        cache = tpq.kv_cache(KL, at, dev)
+        everything = tpq.KvBatch(table, torch.tensor(lens, dtype=torch.int32, device=dev),
+                                 torch.tensor(np.concatenate(([0], np.cumsum(lens))), dtype=torch.int32, device=dev), max_new=max(lens))
+        tpq.kv_append(KL, cache, everything, rnd(sum(lens), heads, D), rnd(sum(lens), heads, D))
+        starts = None if max(new) == 1 else torch.tensor(np.concatenate(([0], np.cumsum(new))), dtype=torch.int32, device=dev)
+        batch = tpq.KvBatch(table, everything.lens, starts, max_new=max(new), max_len=max(lens))
+        tpq.kv_check(KL, cache, batch, T)
+        x, q, o = rnd(T, 3 * heads, D), rnd(T, heads, D), rnd(T, heads, D)
+        msgs = [tpq.Message(L, T, dev) for _ in range(N)]
+        tpq.encode(L, plan, [rnd(T, E) for _ in range(N)], msgs)
+        out = torch.empty((T, E), dtype=torch.bfloat16, device=dev)
+        ws = tpq.kv_attention_workspace(KL, batch, heads, dev)
+        calls = {"append": tpq.kv_append_call(KL, cache, batch, x[:, heads:2 * heads], x[:, 2 * heads:], cos, sin, False, x[:, :heads], q),
+                 "attention": tpq.kv_attention_call(KL, cache, batch, q, o, D ** -0.5, ws),
+                 "gemm_encode": tpq.gemm_encode_call(L, o.view(T, heads * D), Wp, msgs[0]),
+                 "decode_reduce": tpq.decode_reduce_call(L, plan, msgs, out, tpq.ACC_BF16)}
+        us = {k: round(timed([c], 100), 2) for k, c in calls.items()}
+        us["block"] = round(timed(list(calls.values()), 50), 2)
+        graph = torch.cuda.CUDAGraph()
+        want = out.clone()
+        with torch.cuda.graph(graph):
+            for c in calls.values():
+                c()
+        us["block_graph"] = round(timed([graph.replay], 50), 2)
+        if not torch.equal(out, want):
+            sys.exit("kv: the replayed block differs from the eager one")
+        return {"tokens": T, "cached_tokens": sum(lens), "us": us}
+    rng = np.random.default_rng(wl.seed_for(w, 0, 0, 10))
+    return {"section": "attention_block_4bit_cache", "prompt": block([2048], [2048]),
+            "decode": block([int(n) for n in rng.integers(1024, 4097, 64)], [1] * 64),
+            "cache_bytes_per_token": KL.page_bytes // page, "bf16_cache_bytes_per_token": 4 * heads * D}
+
+
 def main():
     ap = argparse.ArgumentParser()
-    ap.add_argument("--sections", default="llama,gemma,large,static,bits,fused,hop,gemm")
+    ap.add_argument("--sections", default="llama,gemma,large,static,bits,fused,hop,gemm,kv")
     ap.add_argument("--only", default="", help="large: only the variants whose name contains this; gemm: only this K "
                                                "(so that a kernel trace holds one shape per kernel)")
     args = ap.parse_args()
@@ -374,7 +433,7 @@ def main():
     import workloads as wl
     table = {"llama": section_llama, "gemma": section_gemma, "large": section_large,
              "static": section_static, "bits": section_bits, "fused": section_fused, "hop": section_hop,
-             "gemm": section_gemm}
+             "gemm": section_gemm, "kv": section_kv}
     for name in args.sections.split(","):
         print(json.dumps(table[name](tpq, wl, args)), flush=True)
 
