@@ -67,6 +67,7 @@ struct KvAttendArgs {
     int32_t window, sinks;
     float scale, softcap;
     int32_t splits;      // 1: no tile of rows is cut; with one sequence: shares of a tile's steps
+    int32_t odd;         // 1: shares of an odd number of steps
     int32_t items, row_tiles, min_tiles;  // items of a head, most tiles of rows of a sequence, least steps of a share
 };
 

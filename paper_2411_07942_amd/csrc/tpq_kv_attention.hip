@@ -176,6 +176,7 @@ __device__ __forceinline__ bool kv_share(const KvArgs &a, const KvAttendArgs &p,
     s.live = 1;
     if (cuts > 1) {
         s.share = max(static_cast<int>(static_cast<uint32_t>(q.most + cuts - 1) / static_cast<uint32_t>(cuts)), p.min_tiles);
+        s.share |= p.odd;
         s.live = max(static_cast<int>(static_cast<uint32_t>(s.span.tiles + s.share - 1) / static_cast<uint32_t>(s.share)), 1);
     }
     return s.split < s.live && s.item0 + s.split < p.items;
@@ -716,10 +717,20 @@ __global__ __launch_bounds__(64 * W, D == 256 ? 1 : 2) void k_kv_attend_many(KvA
 #pragma unroll
         for (int i = 0; i < 4; ++i) c.v[i] = *reinterpret_cast<const uint32_t *>(vs + v_at + i * (D / 2));
     };
-    int base = v0, pages = 0;
+    // (the first pages' numbers of the scan below too: one latency)
+    constexpr int U = NG <= 2 ? 4 : 2, PER = 64 / TOK;  // loads of a lane in flight together, tiles that a wave's lanes cover
+    int base = v0, pages = 0, key[U], id[U];
+    auto scanned = [&](int v) __attribute__((always_inline)) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            key[u] = w.span.tile(min(v + PER * (wave + u * W) + static_cast<int>(ln) / TOK, v1 - 1)) * TOK + static_cast<int>(ln) % TOK;
+            id[u] = table[min(key[u], 16 * n_blocks - 1) >> a.lg_page];
+        }
+    };
     Codes ca = {}, cb = {};
     if (v0 < v1) {
         pages = pages_of(v0);
+        scanned(v0);
         load_codes(ca, v0, v0, base, pages);
         load_codes(cb, v0 + 1, v0 + 1, base, pages);
     }
@@ -732,14 +743,8 @@ __global__ __launch_bounds__(64 * W, D == 256 ? 1 : 2) void k_kv_attend_many(KvA
     {
         if (threadIdx.x < 3) reduced[threadIdx.x] = 0;
         uint32_t top[2] = {0, 0}, missing = 0;
-        constexpr int U = NG <= 2 ? 4 : 2;  // tiles whose loads are in flight together
-        for (int v = v0 + wave; v < v1; v += U * W) {
-            int id[U], key[U];
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                key[u] = w.span.tile(min(v + u * W, v1 - 1)) * TOK + static_cast<int>(ln) % TOK;
-                id[u] = table[min(key[u], 16 * n_blocks - 1) >> a.lg_page];
-            }
+        for (int v = v0; v < v1; v += PER * U * W) {
+            if (v > v0) scanned(v);
             uint32_t x[U][2 * NG];
 #pragma unroll
             for (int u = 0; u < U; ++u) {
@@ -877,7 +882,7 @@ __global__ __launch_bounds__(64 * W, D == 256 ? 1 : 2) void k_kv_attend_many(KvA
         const f16x8_t pb = __builtin_bit_cast(f16x8_t, (u32x4{pw[first], pw[first + 1], pw[first + 2], pw[first + 3]}));
         o[j % DT] = __builtin_amdgcn_mfma_f32_32x32x16_f16(val, pb, o[j % DT], 0, 0, 0);
     };
-    // all of a tile's scores, all of its values: operands read ahead
+    // all of a tile's scores: operands read ahead
     auto all_scores = [&](f32x16 (&acc)[TB], int par) __attribute__((always_inline)) {
         constexpr int A = q_in_lds ? 2 : 4;
         f16x8_t fr[A + 1], fq[A + 1];
@@ -893,18 +898,6 @@ __global__ __launch_bounds__(64 * W, D == 256 ? 1 : 2) void k_kv_attend_many(KvA
                 fq[(i + A) % (A + 1)] = query_at(i + A);
             }
             score(acc, fr[i % (A + 1)], fq[i % (A + 1)], i);
-            __builtin_amdgcn_sched_barrier(0);
-        }
-    };
-    auto all_values = [&](int par) __attribute__((always_inline)) {
-        constexpr int A = q_in_lds ? 2 : 4;
-        f16x8_t fr[A + 1];
-#pragma unroll
-        for (int j = 0; j < A; ++j) fr[j] = value_at(par, j);
-#pragma unroll
-        for (int j = 0; j < NP; ++j) {
-            if (j + A < NP) fr[(j + A) % (A + 1)] = value_at(par, j + A);
-            value(fr[j % (A + 1)], j);
             __builtin_amdgcn_sched_barrier(0);
         }
     };
@@ -950,6 +943,27 @@ __global__ __launch_bounds__(64 * W, D == 256 ? 1 : 2) void k_kv_attend_many(KvA
                 base = v;
                 pages = pages_of(v);
             }
+        };
+        // a tile's values, and in the products' time the codes of the tiles to come
+        auto values_and_codes = [&](auto parity, Codes &codes, int v) __attribute__((always_inline)) {
+            constexpr int P = decltype(parity)::value, Q = P ^ 1, A = q_in_lds ? 2 : 4;
+            f16x8_t fr[A + 1];
+#pragma unroll
+            for (int j = 0; j < A; ++j) fr[j] = value_at(P, j);
+            codes.km = converted(codes.km, k_norm);
+            codes.vm = converted(codes.vm, v_norm);
+            for_each<NP>([&](auto jj) __attribute__((always_inline)) {
+                constexpr int j = decltype(jj)::value;
+                if constexpr (j + A < NP) fr[(j + A) % (A + 1)] = value_at(P, j + A);
+                value(fr[j % (A + 1)], j);
+                for_each<PIECES>([&](auto piece) __attribute__((always_inline)) {
+                    constexpr int x = decltype(piece)::value;
+                    if constexpr (2 * x * NP / (2 * PIECES) == j) store_keys(codes, piece, P);
+                    if constexpr ((2 * x + 1) * NP / (2 * PIECES) == j) store_values(codes, piece, Q);
+                });
+                __builtin_amdgcn_sched_barrier(0);
+            });
+            load_codes(codes, v + 4, v + 3, base, pages);
         };
         // tiles that every row of the workgroup sees whole: steps f0 .. f1 - 1 (but for absent blocks, and for bounded scores)
         const int tile0 = p.window > 0 && w.hi - p.window >= 0 ? (w.hi - p.window) / TOK + 1 : 0, tile1 = w.lo < 0 ? 0 : (w.lo + 1) / TOK;
@@ -1091,15 +1105,8 @@ __global__ __launch_bounds__(64 * W, D == 256 ? 1 : 2) void k_kv_attend_many(KvA
                 }
                 __syncthreads();  // (the keys' buffer is the next one's)
             }
-            const int par = (v - v0) & 1;
-            all_values(par);
-            if (par) {
-                store_codes(cb, 1, 0);
-                load_codes(cb, v + 4, v + 3, base, pages);
-            } else {
-                store_codes(ca, 0, 1);
-                load_codes(ca, v + 4, v + 3, base, pages);
-            }
+            if ((v - v0) & 1) values_and_codes(std::integral_constant<int, 1>{}, cb, v);
+            else values_and_codes(std::integral_constant<int, 0>{}, ca, v);
             __syncthreads();
             ++v;
         }
@@ -1207,13 +1214,19 @@ static KvChoice choose(const KvArgs &a, int D, int R, int reach, int compute_uni
     }
     const int tok = !c.many ? kKvTile : D == 256 ? 32 : 64;
     // at least 128 tokens a share, a step for each wave, or 256 ones that many rows take together
-    c.min_tiles = 128 * (c.many ? 2 : 1) / tok;
+    c.min_tiles = (c.many ? 256 : 128) / tok;
     const int64_t slots = std::max<int64_t>((c.many ? 1 : 3) * compute_units / a.heads, 1);
     const int64_t cuts = std::min<int64_t>(((reach + tok - 1) / tok + 1) / c.min_tiles, 256);
     // Where tiles of rows fill the device uncut, a long sequence among short ones is cut all the same, if there may be one (one
     // of 100 000 tokens among 99 of 200 to 1000, 8 heads: 69 us, uncut 953; 64 equal ones of 8192, 40 heads: 344 and 346).
     const bool always = !c.many && reach >= 8192;
     const auto tiles_of = [&](int rows) { return static_cast<int64_t>((most + rows - 1) / rows); };
+    // One sequence: as many shares as fit; two where its first tiles of rows are so much shorter than its last that they fit anyway
+    // (4096 tokens over themselves, 5 heads: 96 us to 67; 2048, which three shares fit, with six of them 33 to 36).
+    const auto wanted = [&](int64_t groups) {
+        const int64_t seen = static_cast<int64_t>(reach) * 2 - std::min(a.max_new, reach);  // of 2 reach, by an average row
+        return std::max(slots / groups, std::min<int64_t>(c.many ? slots * 2 * reach / (groups * seen) : 0, 2));
+    };
     const auto listed = [&](int64_t groups) { return std::min(std::max(slots, groups + std::max<int64_t>(groups / 2, 1)), groups * cuts); };
     c.row_tiles = tiles_of(c.rows);
     // tiles of rows: no more than the rows there are and one more of each sequence
@@ -1221,7 +1234,7 @@ static KvChoice choose(const KvArgs &a, int D, int R, int reach, int compute_uni
     c.splits = 1;
     c.items = groups;
     if (cuts > 1 && (slots > groups || (always && a.n_seqs > 1))) {
-        c.splits = a.n_seqs > 1 ? 2 : std::max<int64_t>(std::min(slots / groups, cuts), 1);
+        c.splits = a.n_seqs > 1 ? 2 : std::max<int64_t>(std::min(wanted(groups), cuts), 1);
         c.items = a.n_seqs > 1 ? listed(groups) : groups * c.splits;
     }
     // (fewer rows than sequences times max_new may leave room for shares; tiles of 256 rows fill the device uncut)
@@ -1229,7 +1242,7 @@ static KvChoice choose(const KvArgs &a, int D, int R, int reach, int compute_uni
     if (cuts > 1) {
         const int rows = c.many ? 128 : c.rows;
         const int64_t top = std::min(a.n_seqs * tiles_of(rows), always ? INT64_MAX : slots - 1);
-        if (top > 0) c.partial_rows = static_cast<size_t>(a.heads) * rows * std::max(listed(top), std::min(slots, top * cuts));
+        if (top > 0) c.partial_rows = static_cast<size_t>(a.heads) * rows * std::max(listed(top), std::min(c.many ? 2 * slots : slots, top * cuts));
     }
     return c;
 }
@@ -1308,9 +1321,11 @@ int launch_kv_attend(const KvArgs &a, KvAttendArgs p, int D, int max_len, void *
     p.items = c.items;
     p.row_tiles = c.row_tiles;
     p.min_tiles = c.min_tiles;
+    p.odd = c.many;
     p.part = static_cast<float *>(workspace);
     p.part_ml = p.part + static_cast<size_t>(a.heads) * c.items * c.rows * D;
     if (c.items * a.heads > kKvMaxItems) return TPQ_ERR_SHAPE;
+    if (c.splits > 1 && static_cast<uint64_t>(c.items) * a.heads * c.rows > choose(a, D, p.R, max_len, cu).partial_rows) return TPQ_ERR_WORKSPACE;
     const dim3 grid(static_cast<uint32_t>(c.items) * a.heads);
     if (c.many) {
         e = D == 256 ? launch_many_of<256, 4, 32>(a, p, grid, s)
