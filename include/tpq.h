@@ -431,9 +431,9 @@ int tpq_kv_read(const tpq_kv_layout *L, const void *cache, const tpq_kv_batch *b
  *     s_j = scale * q . k_j;  softcap > 0: s_j = softcap * tanh(s_j / softcap)
  *     out = sum_j exp(s_j) v_j / sum_j exp(s_j)        over the keys it sees; none: 0
  * with k_j, v_j the cache's values.  Scores, exponentials' sums and accumulators are fp32.
- * With up to 32 rows of a head (max_new * q_heads / L.heads) per sequence, 8 where D = 8 G, the
- * products take the codes themselves, which are exact in bf16, and the probabilities as pairs of bf16
- * (17 bits); with more, keys and values are rounded to fp16 at a scale of their own and so are the probabilities (2^-12).
+ * With up to 64 rows of a head (max_new * q_heads / L.heads) per sequence, 32 where D = 4 G and 8 where
+ * D = 8 G, the products take the codes themselves, which are exact in bf16, and the probabilities as
+ * pairs of bf16 (17 bits); with more, keys and values are rounded to fp16 at a scale of their own and so are the probabilities (2^-12).
  *     Q, out    [device] bf16 [rows][ldQ], [rows][ldOut], elements, multiples of 8
  *     window, sinks  >= 0, at most 2^28 (sinks without a window change nothing)
  *     workspace [device] >= tpq_kv_attention_workspace_bytes(..) bytes (which depends on L, the batch's

@@ -246,14 +246,13 @@ struct KvRaw {
     bool bad[2];             // (uniform) a page that is none
 };
 
-template <int D, int GROUPS, int NR, bool COLS>
-__global__ __launch_bounds__(256, D * NR <= 128 && (COLS || GROUPS <= 2) ? 3 : 2) void k_kv_attend_few(KvArgs a, KvAttendArgs p)
+template <int D, int GROUPS, bool COLS>
+__global__ __launch_bounds__(256, D <= 128 && (COLS || GROUPS <= 2) ? 3 : 2) void k_kv_attend_few(KvArgs a, KvAttendArgs p)
 {
     constexpr int NG = COLS ? 1 : GROUPS;  // groups one after the other
-    constexpr int KK = D / 32, NT = D / 16, KPG = KK / NG, TPG = NT / NG, ROWS = COLS ? 16 / GROUPS : 16 * NR;
+    constexpr int KK = D / 32, NT = D / 16, KPG = KK / NG, TPG = NT / NG, ROWS = COLS ? 16 / GROUPS : 16;
     constexpr int RW = COLS ? 16 / GROUPS : 16;  // columns of a group
     typedef KvRaw<D, GROUPS, COLS> Raw;
-    static_assert(!COLS || NR == 1, "rows");
     __shared__ float sO[2][ROWS][D + 4];
     __shared__ float sM[2][ROWS], sL[2][ROWS];
     const CodePair code_pair;
@@ -270,30 +269,24 @@ __global__ __launch_bounds__(256, D * NR <= 128 && (COLS || GROUPS <= 2) ? 3 : 2
 
     // queries: column m of the products' right operand; COLS: column RW gr + r has row r's features of group gr
     const uint32_t mr = m % RW, mg = m / RW;
-    bf16x8_t q[NR][KK];
-    float qs[NR][NG];
-    int pos[NR];
+    bf16x8_t q[KK];
+    float qs[NG];
+    const int row = rt * ROWS + static_cast<int>(mr), rc = min(row, n_rows - 1), i = p.by_R.of(rc), pos = base + i;
+    const uint8_t *src = p.Q + (row0 + i) * p.ldQ + (h * p.R + rc - i * p.R) * (2 * D) + 16 * g;
 #pragma unroll
-    for (int r = 0; r < NR; ++r) {
-        const int row = rt * ROWS + 16 * r + static_cast<int>(mr);
-        const int rc = min(row, n_rows - 1), i = p.by_R.of(rc);
-        pos[r] = base + i;
-        const uint8_t *src = p.Q + (row0 + i) * p.ldQ + (h * p.R + rc - i * p.R) * (2 * D) + 16 * g;
+    for (int gr = 0; gr < NG; ++gr) {
+        float sum = 0.0f;
 #pragma unroll
-        for (int gr = 0; gr < NG; ++gr) {
-            float sum = 0.0f;
+        for (int kk = gr * KPG; kk < (gr + 1) * KPG; ++kk) {
+            u32x4 w = *reinterpret_cast<const u32x4 *>(src + 64 * kk);
+            if (p.scale < 0.0f) w ^= 0x80008000u;  // (scores are then multiplied by |scale|: their order is the products')
+            if (COLS && static_cast<uint32_t>(kk * GROUPS / KK) != mg) w = u32x4{0, 0, 0, 0};
+            q[kk] = __builtin_bit_cast(bf16x8_t, w);
+            const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
-            for (int kk = gr * KPG; kk < (gr + 1) * KPG; ++kk) {
-                u32x4 w = *reinterpret_cast<const u32x4 *>(src + 64 * kk);
-                if (p.scale < 0.0f) w ^= 0x80008000u;  // (scores are then multiplied by |scale|: their order is the products')
-                if (COLS && static_cast<uint32_t>(kk * GROUPS / KK) != mg) w = u32x4{0, 0, 0, 0};
-                q[r][kk] = __builtin_bit_cast(bf16x8_t, w);
-                const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-                for (int e = 0; e < 4; ++e) sum += bf16_lo_to_f32(ws[e]) + bf16_hi_to_f32(ws[e]);
-            }
-            qs[r][gr] = group4_sum(sum);
+            for (int e = 0; e < 4; ++e) sum += bf16_lo_to_f32(ws[e]) + bf16_hi_to_f32(ws[e]);
         }
+        qs[gr] = group4_sum(sum);
     }
 
     const int n_blocks = (min(len, a.ld_table << a.lg_page) + 15) / 16;  // blocks of 16 tokens that exist
@@ -344,18 +337,13 @@ __global__ __launch_bounds__(256, D * NR <= 128 && (COLS || GROUPS <= 2) ? 3 : 2
         }
     };
 
-    f32x4 o[NR][NT], oc[NR];  // accumulators; row gr of oc: 128 * (sum of group gr's weights as the products see them)
-    float zs[NR][NG], mx[NR], l[NR];
+    f32x4 o[NT], oc;  // accumulators; row gr of oc: 128 * (sum of group gr's weights as the products see them)
+    float zs[NG], mx = kKvLowest, l = 0.0f;
 #pragma unroll
-    for (int r = 0; r < NR; ++r) {
-        mx[r] = kKvLowest;
-        l[r] = 0.0f;
+    for (int t = 0; t < NT; ++t) o[t] = f32x4{0, 0, 0, 0};
+    oc = f32x4{0, 0, 0, 0};
 #pragma unroll
-        for (int t = 0; t < NT; ++t) o[r][t] = f32x4{0, 0, 0, 0};
-        oc[r] = f32x4{0, 0, 0, 0};
-#pragma unroll
-        for (int gr = 0; gr < NG; ++gr) zs[r][gr] = 0.0f;
-    }
+    for (int gr = 0; gr < NG; ++gr) zs[gr] = 0.0f;
     const float log2e = 1.44269504f;
 
     // scores in powers of two: exp(s) = 2^(s log2 e)
@@ -384,132 +372,112 @@ __global__ __launch_bounds__(256, D * NR <= 128 && (COLS || GROUPS <= 2) ? 3 : 2
     auto step = [&](const Raw &raw, int v) {
         const int t0 = span.tile(v) * kKvTile;
         const bool whole = t0 + kKvTile - 1 <= lo && (p.window == 0 || t0 > hi - p.window || t0 + kKvTile <= p.sinks) && !raw.bad[0] && !raw.bad[1];
-        float s[NR][2][4];
-        bool vis[NR][2][4];
+        float s[2][4];
+        bool vis[2][4];
         for_each<2>([&](auto jj) {
             constexpr int J = decltype(jj)::value;
 #pragma unroll
             for (int gr = 0; gr < NG; ++gr) {
-                f32x4 acc[NR];
-#pragma unroll
-                for (int r = 0; r < NR; ++r) {
-                    float c0 = -128.0f * qs[r][gr];
-                    asm volatile("" : "+v"(c0));  // (anew in every step: kept outside the loop it would take four registers)
-                    acc[r] = f32x4{c0, c0, c0, c0};
-                }
+                float c0 = -128.0f * qs[gr];
+                asm volatile("" : "+v"(c0));  // (anew in every step: kept outside the loop it would take four registers)
+                f32x4 acc = {c0, c0, c0, c0};
 #pragma unroll
                 for (int kk = gr * KPG; kk < (gr + 1) * KPG; ++kk) {
                     const uint32_t w = raw.k[J][kk];
                     const u32x4 c = {code_pair(w), code_pair(w >> 4), code_pair(w >> 8), code_pair(w >> 12)};
-#pragma unroll
-                    for (int r = 0; r < NR; ++r)
-                        acc[r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, c), q[r][kk], acc[r], 0, 0, 0);
+                    acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, c), q[kk], acc, 0, 0, 0);
                 }
                 float sc[Raw::META], ze[Raw::META];
                 metas_of(raw, gr, sc, ze);
                 for_each<4>([&](auto i) {
                     constexpr int I = decltype(i)::value;
                     // (products, whose operand the exchange goes into; multiply-adds would take a move for each)
-#pragma unroll
-                    for (int r = 0; r < NR; ++r) {
-                        const float x = meta_of(of_keys, jj, i, sc, gr) * acc[r][I], z = meta_of(of_keys, jj, i, ze, gr) * qs[r][gr];
-                        s[r][J][I] = gr == 0 ? x + z : (s[r][J][I] + x) + z;
-                        // the groups' parts (in an order that leaves the same sum in all of them)
-                        if (COLS && RW <= 8) s[r][J][I] += dpp_f32<0x128>(s[r][J][I]);
-                        if (COLS && RW <= 4) s[r][J][I] += dpp_f32<0x124>(s[r][J][I]);
-                        if (COLS && RW <= 2) s[r][J][I] += dpp_f32<0x122>(s[r][J][I]);
-                    }
+                    const float x = meta_of(of_keys, jj, i, sc, gr) * acc[I], z = meta_of(of_keys, jj, i, ze, gr) * qs[gr];
+                    s[J][I] = gr == 0 ? x + z : (s[J][I] + x) + z;
+                    // the groups' parts (in an order that leaves the same sum in all of them)
+                    if (COLS && RW <= 8) s[J][I] += dpp_f32<0x128>(s[J][I]);
+                    if (COLS && RW <= 4) s[J][I] += dpp_f32<0x124>(s[J][I]);
+                    if (COLS && RW <= 2) s[J][I] += dpp_f32<0x122>(s[J][I]);
                 });
             }
         });
-#pragma unroll
-        for (int r = 0; r < NR; ++r) {
-            if (p.softcap > 0.0f) {
-#pragma unroll
-                for (int x = 0; x < 8; ++x) {
-                    // cap tanh(x / cap) = cap - 2 cap / (exp(2 x / cap) + 1)
-                    const float e = __builtin_amdgcn_exp2f(s[r][x >> 2][x & 3] * cap_in) + 1.0f;
-                    s[r][x >> 2][x & 3] = __builtin_fmaf(-2.0f * cap_out, __builtin_amdgcn_rcpf(e), cap_out);
-                }
-            }
-            if (!whole) {
-#pragma unroll
-                for (int x = 0; x < 8; ++x) {
-                    const int j = x >> 2, i = x & 3, key = t0 + 16 * j + 4 * static_cast<int>(g) + i;
-                    vis[r][j][i] = (key <= pos[r]) & ((key > pos[r] - window) | (key < p.sinks)) & !raw.bad[j] & (key < 16 * n_blocks);
-                    s[r][j][i] = vis[r][j][i] ? s[r][j][i] : kKvLowest;
-                }
-            }
-            float top = s[r][0][0];
-#pragma unroll
-            for (int x = 1; x < 8; ++x) top = fmaxf(top, s[r][x >> 2][x & 3]);
-            top *= k_score;
-            // The maximum only follows where a weight would pass 2^8: weights are relative anyway, and a step without it saves
-            // the accumulators' rescaling.
-            if (__builtin_amdgcn_ballot_w64(top > mx[r] + 8.0f)) {
-                const float now = fmaxf(mx[r], group4_max(top)), alpha = __builtin_amdgcn_exp2f(mx[r] - now);
-                mx[r] = now;
-                l[r] *= alpha;
-#pragma unroll
-                for (int t = 0; t < NT; ++t) o[r][t] *= alpha;
-                oc[r] *= alpha;
-#pragma unroll
-                for (int gr = 0; gr < NG; ++gr) zs[r][gr] *= alpha;
-            }
+        if (p.softcap > 0.0f) {
 #pragma unroll
             for (int x = 0; x < 8; ++x) {
-                float &e = s[r][x >> 2][x & 3];  // the weight, in the score's place
-                e = __builtin_amdgcn_exp2f(__builtin_fmaf(e, k_score, -mx[r]));
-                if (!whole) e = vis[r][x >> 2][x & 3] ? e : 0.0f;
-                l[r] += e;
+                // cap tanh(x / cap) = cap - 2 cap / (exp(2 x / cap) + 1)
+                const float e = __builtin_amdgcn_exp2f(s[x >> 2][x & 3] * cap_in) + 1.0f;
+                s[x >> 2][x & 3] = __builtin_fmaf(-2.0f * cap_out, __builtin_amdgcn_rcpf(e), cap_out);
             }
+        }
+        if (!whole) {
+#pragma unroll
+            for (int x = 0; x < 8; ++x) {
+                const int j = x >> 2, i = x & 3, key = t0 + 16 * j + 4 * static_cast<int>(g) + i;
+                vis[j][i] = (key <= pos) & ((key > pos - window) | (key < p.sinks)) & !raw.bad[j] & (key < 16 * n_blocks);
+                s[j][i] = vis[j][i] ? s[j][i] : kKvLowest;
+            }
+        }
+        float top = s[0][0];
+#pragma unroll
+        for (int x = 1; x < 8; ++x) top = fmaxf(top, s[x >> 2][x & 3]);
+        top *= k_score;
+        // The maximum only follows where a weight would pass 2^8: weights are relative anyway, and a step without it saves
+        // the accumulators' rescaling.
+        if (__builtin_amdgcn_ballot_w64(top > mx + 8.0f)) {
+            const float now = fmaxf(mx, group4_max(top)), alpha = __builtin_amdgcn_exp2f(mx - now);
+            mx = now;
+            l *= alpha;
+#pragma unroll
+            for (int t = 0; t < NT; ++t) o[t] *= alpha;
+            oc *= alpha;
+#pragma unroll
+            for (int gr = 0; gr < NG; ++gr) zs[gr] *= alpha;
+        }
+#pragma unroll
+        for (int x = 0; x < 8; ++x) {
+            float &e = s[x >> 2][x & 3];  // the weight, in the score's place
+            e = __builtin_amdgcn_exp2f(__builtin_fmaf(e, k_score, -mx));
+            if (!whole) e = vis[x >> 2][x & 3] ? e : 0.0f;
+            l += e;
         }
 #pragma unroll
         for (int gr = 0; gr < NG; ++gr) {
-            bf16x8_t bh[NR], bl[NR];
             float sc[Raw::META], ze[Raw::META];
             metas_of(raw, gr, sc, ze);
-#pragma unroll
-            for (int r = 0; r < NR; ++r) {
-                u32x4 ph, pl;
-                for_each<2>([&](auto jj) {
-                    constexpr int J = decltype(jj)::value;
-                    float w[4];
+            u32x4 ph, pl;
+            for_each<2>([&](auto jj) {
+                constexpr int J = decltype(jj)::value;
+                float w[4];
+                for_each<4>([&](auto i) {
+                    constexpr int I = decltype(i)::value;
+                    w[I] = meta_of(of_values, jj, i, sc, gr) * s[J][I];
+                });
+                if (whole) {
                     for_each<4>([&](auto i) {
                         constexpr int I = decltype(i)::value;
-                        w[I] = meta_of(of_values, jj, i, sc, gr) * s[r][J][I];
+                        zs[gr] += meta_of(of_values, jj, i, ze, gr) * s[J][I];
                     });
-                    if (whole) {
-                        for_each<4>([&](auto i) {
-                            constexpr int I = decltype(i)::value;
-                            zs[r][gr] += meta_of(of_values, jj, i, ze, gr) * s[r][J][I];
-                        });
-                    } else {  // (what lies behind a hidden key may be anything)
-                        for_each<4>([&](auto i) {
-                            constexpr int I = decltype(i)::value;
-                            const float z = meta_of(of_values, jj, i, ze, gr) * s[r][J][I];
-                            zs[r][gr] += vis[r][J][I] ? z : 0.0f;
-                            w[I] = vis[r][J][I] ? w[I] : 0.0f;
-                        });
-                    }
+                } else {  // (what lies behind a hidden key may be anything)
+                    for_each<4>([&](auto i) {
+                        constexpr int I = decltype(i)::value;
+                        const float z = meta_of(of_values, jj, i, ze, gr) * s[J][I];
+                        zs[gr] += vis[J][I] ? z : 0.0f;
+                        w[I] = vis[J][I] ? w[I] : 0.0f;
+                    });
+                }
 #pragma unroll
-                    for (int i = 0; i < 4; i += 2) {
-                        const uint32_t hi2 = pack_bf16x2(w[i], w[i + 1]);
-                        ph[2 * J + i / 2] = hi2;
-                        pl[2 * J + i / 2] = pack_bf16x2(w[i] - bf16_lo_to_f32(hi2), w[i + 1] - bf16_hi_to_f32(hi2));
-                    }
-                });
-                bh[r] = __builtin_bit_cast(bf16x8_t, ph);
-                bl[r] = __builtin_bit_cast(bf16x8_t, pl);
-            }
+                for (int i = 0; i < 4; i += 2) {
+                    const uint32_t hi2 = pack_bf16x2(w[i], w[i + 1]);
+                    ph[2 * J + i / 2] = hi2;
+                    pl[2 * J + i / 2] = pack_bf16x2(w[i] - bf16_lo_to_f32(hi2), w[i + 1] - bf16_hi_to_f32(hi2));
+                }
+            });
+            const bf16x8_t bh = __builtin_bit_cast(bf16x8_t, ph), bl = __builtin_bit_cast(bf16x8_t, pl);
             uint32_t one = NG == 1 || m == static_cast<uint32_t>(gr) ? code_pair.base : 0u;
             if (NG > 1) asm volatile("" : "+v"(one));
             const bf16x8_t ones = __builtin_bit_cast(bf16x8_t, (u32x4{one, one, one, one}));
-#pragma unroll
-            for (int r = 0; r < NR; ++r) {
-                oc[r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, bh[r], oc[r], 0, 0, 0);
-                oc[r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, bl[r], oc[r], 0, 0, 0);
-            }
+            oc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, bh, oc, 0, 0, 0);
+            oc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, bl, oc, 0, 0, 0);
 #pragma unroll
             for (int t = gr * TPG; t < (gr + 1) * TPG; ++t) {
                 const int word = t / 8, byte = (t % 8) / 2;
@@ -523,11 +491,8 @@ __global__ __launch_bounds__(256, D * NR <= 128 && (COLS || GROUPS <= 2) ? 3 : 2
                     c[x] = code_pair(t & 1 ? y >> 4 : y);
                 }
                 const bf16x8_t av = __builtin_bit_cast(bf16x8_t, c);
-#pragma unroll
-                for (int r = 0; r < NR; ++r) {
-                    o[r][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av, bh[r], o[r][t], 0, 0, 0);
-                    o[r][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av, bl[r], o[r][t], 0, 0, 0);
-                }
+                o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av, bh, o[t], 0, 0, 0);
+                o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av, bl, o[t], 0, 0, 0);
             }
             if (NG > 1) __builtin_amdgcn_sched_barrier(0);  // (one group's codes and weights in registers at a time)
         }
@@ -557,15 +522,12 @@ __global__ __launch_bounds__(256, D * NR <= 128 && (COLS || GROUPS <= 2) ? 3 : 2
     }
 
     // 128 * (sum of the weights) off the codes, the zeros' share on
+    l = group4_sum(l);
 #pragma unroll
-    for (int r = 0; r < NR; ++r) {
-        l[r] = group4_sum(l[r]);
+    for (int gr = 0; gr < NG; ++gr) {
+        const float z = group4_sum(zs[gr]), c = NG == 1 ? oc[0] : __shfl(oc[gr & 3], 16 * (gr >> 2) + m, 64);
 #pragma unroll
-        for (int gr = 0; gr < NG; ++gr) {
-            const float z = group4_sum(zs[r][gr]), c = NG == 1 ? oc[r][0] : __shfl(oc[r][gr & 3], 16 * (gr >> 2) + m, 64);
-#pragma unroll
-            for (int t = gr * TPG; t < (gr + 1) * TPG; ++t) o[r][t] = o[r][t] - c + z;
-        }
+        for (int t = gr * TPG; t < (gr + 1) * TPG; ++t) o[t] = o[t] - c + z;
     }
     // (COLS: a lane's accumulators are its column's, of which those of its own group count)
     const auto mine = [&](int t) { return !COLS || static_cast<uint32_t>(t * GROUPS / NT) == mg; };
@@ -574,51 +536,40 @@ __global__ __launch_bounds__(256, D * NR <= 128 && (COLS || GROUPS <= 2) ? 3 : 2
     for (int from = 2; from >= 1; from >>= 1) {
         if (wave >= from && wave < 2 * from) {
 #pragma unroll
-            for (int r = 0; r < NR; ++r) {
-#pragma unroll
-                for (int t = 0; t < NT; ++t)
-                    if (mine(t)) *reinterpret_cast<f32x4 *>(&sO[wave - from][16 * r + mr][16 * t + 4 * g]) = o[r][t];
-                if (g == 0 && mg == 0) {
-                    sM[wave - from][16 * r + mr] = mx[r];
-                    sL[wave - from][16 * r + mr] = l[r];
-                }
+            for (int t = 0; t < NT; ++t)
+                if (mine(t)) *reinterpret_cast<f32x4 *>(&sO[wave - from][mr][16 * t + 4 * g]) = o[t];
+            if (g == 0 && mg == 0) {
+                sM[wave - from][mr] = mx;
+                sL[wave - from][mr] = l;
             }
         }
         __syncthreads();
         if (wave < from) {
+            const float m2 = sM[wave][mr], now = fmaxf(mx, m2);
+            const float f1 = __builtin_amdgcn_exp2f(mx - now), f2 = __builtin_amdgcn_exp2f(m2 - now);
+            mx = now;
+            l = l * f1 + sL[wave][mr] * f2;
 #pragma unroll
-            for (int r = 0; r < NR; ++r) {
-                const float m2 = sM[wave][16 * r + mr], now = fmaxf(mx[r], m2);
-                const float f1 = __builtin_amdgcn_exp2f(mx[r] - now), f2 = __builtin_amdgcn_exp2f(m2 - now);
-                mx[r] = now;
-                l[r] = l[r] * f1 + sL[wave][16 * r + mr] * f2;
-#pragma unroll
-                for (int t = 0; t < NT; ++t)
-                    if (mine(t)) o[r][t] = o[r][t] * f1 + *reinterpret_cast<const f32x4 *>(&sO[wave][16 * r + mr][16 * t + 4 * g]) * f2;
-            }
+            for (int t = 0; t < NT; ++t)
+                if (mine(t)) o[t] = o[t] * f1 + *reinterpret_cast<const f32x4 *>(&sO[wave][mr][16 * t + 4 * g]) * f2;
         }
         __syncthreads();
     }
-    if (wave != 0) return;
+    if (wave != 0 || row >= n_rows) return;
+    if (live == 1) {
+        const int i = p.by_R.of(row);
+        uint8_t *dst = p.out + (row0 + i) * p.ldOut + (h * p.R + row - i * p.R) * (2 * D) + 8 * g;
+        const float inv = l > 0.0f ? 1.0f / l : 0.0f;
 #pragma unroll
-    for (int r = 0; r < NR; ++r) {
-        const int row = rt * ROWS + 16 * r + static_cast<int>(mr);
-        if (row >= n_rows) continue;
-        if (live == 1) {
-            const int i = p.by_R.of(row);
-            uint8_t *dst = p.out + (row0 + i) * p.ldOut + (h * p.R + row - i * p.R) * (2 * D) + 8 * g;
-            const float inv = l[r] > 0.0f ? 1.0f / l[r] : 0.0f;
+        for (int t = 0; t < NT; ++t)
+            if (mine(t)) *reinterpret_cast<uint2 *>(dst + 32 * t) = make_uint2(pack_bf16x2(o[t][0] * inv, o[t][1] * inv), pack_bf16x2(o[t][2] * inv, o[t][3] * inv));
+    } else {
+        const int64_t at = (h * static_cast<int64_t>(p.items) + w.item0 + split) * ROWS + mr;
+        float *dst = p.part + at * D + 4 * g;
 #pragma unroll
-            for (int t = 0; t < NT; ++t)
-                if (mine(t)) *reinterpret_cast<uint2 *>(dst + 32 * t) = make_uint2(pack_bf16x2(o[r][t][0] * inv, o[r][t][1] * inv), pack_bf16x2(o[r][t][2] * inv, o[r][t][3] * inv));
-        } else {
-            const int64_t at = (h * static_cast<int64_t>(p.items) + w.item0 + split) * ROWS + 16 * r + mr;
-            float *dst = p.part + at * D + 4 * g;
-#pragma unroll
-            for (int t = 0; t < NT; ++t)
-                if (mine(t)) *reinterpret_cast<f32x4 *>(dst + 16 * t) = o[r][t];
-            if (g == 0 && mg == 0) *reinterpret_cast<float2 *>(p.part_ml + 2 * at) = make_float2(mx[r], l[r]);
-        }
+        for (int t = 0; t < NT; ++t)
+            if (mine(t)) *reinterpret_cast<f32x4 *>(dst + 16 * t) = o[t];
+        if (g == 0 && mg == 0) *reinterpret_cast<float2 *>(p.part_ml + 2 * at) = make_float2(mx, l);
     }
 }
 
@@ -1197,15 +1148,16 @@ static KvChoice choose(const KvArgs &a, int D, int R, int reach, int compute_uni
 {
     KvChoice c;
     const int most = a.max_new * R;  // rows of a head and sequence
-    // The few rows' kernel reads the cache once for 16 of them, or for 32; the other one dequantises every tile, for 128 or 256 (16
-    // sequences of 4096 tokens, 8 heads of 128: 32 rows 39 us to the other's 55, 64 rows 64 to 58; 4 groups 52 to 63, 98 to 64).
-    // Of 8 groups it takes two rows at once (heads of 256: 4 rows 72 us to 135, 8 rows 118 to 136, 16 rows 214 to 136).
-    c.many = most > (a.ng == 8 ? 8 : 32);
+    // The few rows' kernel reads the cache once for 16 of them, the other one dequantises every tile, for 128 or 256 (16 sequences of
+    // 4096 tokens, 8 heads of 128: 64 rows 46 us to 61, with two groups 55 to 64, with four 98 to 64; 96 rows 78 to 64; 64 tokens alone,
+    // 40 heads: 5.8 to 10.2).  Four groups: 32 rows 52 us to 63.  Of 8 groups it takes two rows at once (heads of 256: 4 rows 72 us to
+    // 135, 8 rows 118 to 136, 16 rows 214 to 136).
+    c.many = most > (a.ng <= 2 ? 64 : a.ng == 4 ? 32 : 8);
     // A column for each row and group: one accumulation for all groups, but only 16 / ng rows a tile.  Two tiles of it are still
     // faster than one of 16 rows whose groups come one after the other if those are 4 (8 rows of heads of 128: 35 us to 40, 16 rows 62
     // to 42), not if they are 2 (16 rows 35 to 28); with heads of 256 and 4 groups the latter lacks registers (16 rows 91 to 151).
     c.cols = a.ng > 1 && !c.many && (a.ng == 8 || (D == 256 && a.ng == 4) || most * a.ng <= (a.ng == 4 ? 32 : 16));
-    c.rows = c.many ? 128 : c.cols ? 16 / a.ng : most > 16 && D <= 128 && a.ng == 1 ? 32 : 16;
+    c.rows = c.many ? 128 : c.cols ? 16 / a.ng : 16;
     // 256 rows a workgroup dequantise a tile half as often as 128, if they fill the device and are most of a tile (4096 tokens over
     // 16384, 32 heads: 1060 us and 1110; 2048 over 2048, 5 heads, which do not: 38 and 36).
     if (c.many && D <= 128) {
@@ -1258,12 +1210,12 @@ template <int D>
 static auto few_kernel(int ng, bool cols)
 {
     if constexpr (D == 256) {
-        if (ng == 8) return k_kv_attend_few<D, 8, 1, true>;
-        if (ng == 4) return k_kv_attend_few<D, 4, 1, true>;
+        if (ng == 8) return k_kv_attend_few<D, 8, true>;
+        if (ng == 4) return k_kv_attend_few<D, 4, true>;
     }
     if constexpr (D == 128)
-        if (ng == 4) return cols ? k_kv_attend_few<D, 4, 1, true> : k_kv_attend_few<D, 4, 1, false>;
-    return ng == 1 ? k_kv_attend_few<D, 1, 1, false> : cols ? k_kv_attend_few<D, 2, 1, true> : k_kv_attend_few<D, 2, 1, false>;
+        if (ng == 4) return cols ? k_kv_attend_few<D, 4, true> : k_kv_attend_few<D, 4, false>;
+    return ng == 1 ? k_kv_attend_few<D, 1, false> : cols ? k_kv_attend_few<D, 2, true> : k_kv_attend_few<D, 2, false>;
 }
 
 // Two tiles of keys and of values, heads of 256 their queries too: more than the default limit of LDS, allowed once per device.
@@ -1334,8 +1286,7 @@ int launch_kv_attend(const KvArgs &a, KvAttendArgs p, int D, int max_len, void *
         if (e != hipSuccess) return hip_result(e);
     } else {
         const auto kernel = D == 256 ? few_kernel<256>(a.ng, c.cols)
-                            : c.rows == 32 ? (D == 64 ? k_kv_attend_few<64, 1, 2, false> : k_kv_attend_few<128, 1, 2, false>)
-                                           : (D == 64 ? few_kernel<64>(a.ng, c.cols) : few_kernel<128>(a.ng, c.cols));
+                            : (D == 64 ? few_kernel<64>(a.ng, c.cols) : few_kernel<128>(a.ng, c.cols));
         launch_kernel(kernel, grid, dim3(256), 0, s, a, p);
     }
     if (c.splits > 1) {

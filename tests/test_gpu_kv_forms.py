@@ -68,6 +68,11 @@ LISTED = [  # lens, new, heads, R, D, G, page, window
     ([2100, 600, 40], [40, 37, 40], 1, 2, 256, 128, 16, 0),
     ([3000, 2800], [34, 50], 1, 1, 64, 32, 64, 1500),
     (lengths(75, 40, 600, 11), lengths(75, 0, 40, 12), 1, 2, 128, 64, 16, 0),
+    ([3000, 2800], [70, 66], 1, 1, 64, 32, 64, 1500),
+    # tiles of 16 rows, up to 64 of them
+    ([900, 2000, 40], [64, 1, 40], 2, 1, 128, 128, 16, 0),
+    ([900, 2000, 40], [15, 16, 9], 1, 4, 256, 128, 32, 500),
+    ([64, 50], [64, 50], 3, 1, 64, 64, 16, 0),
 ]
 
 
