@@ -59,7 +59,7 @@
  *     are re-entrant across streams (tpq_calibrate_fixed: see there).
  *   - Work is enqueued on the given HIP stream (a hipStream_t passed as void*,
  *     NULL = the default stream) and the call returns without synchronising,
- *     except tpq_plan_check.
+ *     except tpq_plan_check and tpq_kv_check.
  *   - Inputs must be finite.  NaN / Inf give unspecified values, never a fault.
  *   - T = 0 (or S = 0) is a successful no-op.
  */
@@ -127,7 +127,7 @@ int tpq_last_hip_error(void); /* hipError_t of the most recent TPQ_ERR_HIP on th
 
 /* Measurement aid (for benchmarks: no part of the method).  The next kernel that
  * tpq_encode, tpq_hop, tpq_encode_static, tpq_decode_reduce, tpq_decode_reduce_fused or
- * tpq_decode_reduce_static (or tpq_gemm_encode) launches from the calling thread carries the two HIP events
+ * tpq_decode_reduce_static (or tpq_gemm_encode, tpq_kv_append, tpq_kv_read, tpq_kv_attention) launches from the calling thread carries the two HIP events
  * (hipEvent_t passed as void*, created by the caller with timing enabled) on its own
  * dispatch: afterwards hipEventElapsedTime(start, stop) is that kernel's duration on
  * the GPU, without the idle time that separately recorded events put around a launch.
@@ -364,7 +364,8 @@ int tpq_decode_reduce_static(const tpq_layout *L, const void *plan, int n_ranks,
  * these host numbers.  Nothing outside the buffers is ever touched: a sequence whose starts lie
  * outside 0..rows or decrease is left out (others of such a batch may be, too), a token whose page number is outside 0..n_pages - 1, or
  * whose position is outside the table, counts as absent: not written, not read, not seen.
- * tpq_kv_check reports all of these. */
+ * tpq_kv_check reports all of these.  Matrices whose rows would take 2^32 threads or more are
+ * refused (TPQ_ERR_SHAPE). */
 #define TPQ_KV_MAX_HEADS 256
 
 typedef struct tpq_kv_layout {

@@ -7,7 +7,7 @@
 // come from: one launch serves a step.  A workgroup takes 16 tokens (8 with heads of 256) of one or four columns of units: side by
 // side in a page, their scales, 4 bytes a token, fill a line of one XCD's cache, where tokens of different XCDs would each write back
 // theirs (a batch of 37 ragged prompts, 16 900 tokens, heads of 64: append and read 79 us by sequence and token, 66 so).
-// Bound by memory: 184 + 80 MB there, 4.0 TB/s; small calls by the chain of loads arguments, starts, table, codes.
+// Bound by memory: 295 MB there, 4.5 TB/s; small calls by the chain of loads arguments, starts, table, codes.
 #include "tpq_device.h"
 #include "tpq_kv.h"
 
