@@ -438,7 +438,7 @@ int tpq_kv_read(const tpq_kv_layout *L, const void *cache, const tpq_kv_batch *b
  *     Q, out    [device] bf16 [rows][ldQ], [rows][ldOut], elements, multiples of 8
  *     window, sinks  >= 0, at most 2^28 (sinks without a window change nothing)
  *     workspace [device] >= tpq_kv_attention_workspace_bytes(..) bytes (which depends on L, the batch's
- *               host numbers, q_heads and the current device's compute units), 16-byte aligned,
+ *               host numbers but rows, q_heads and the current device's compute units), 16-byte aligned,
  *               contents arbitrary; calls that share a workspace must not overlap in time */
 size_t tpq_kv_attention_workspace_bytes(const tpq_kv_layout *L, const tpq_kv_batch *batch, int q_heads);
 int tpq_kv_attention(const tpq_kv_layout *L, const void *cache, const tpq_kv_batch *batch,

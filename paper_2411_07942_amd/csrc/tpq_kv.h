@@ -60,6 +60,7 @@ struct KvAttendArgs {
     const uint8_t *Q;
     uint8_t *out;
     int64_t ldQ, ldOut;  // bytes
+    int32_t *plan;       // the list of items, of more than 64 sequences
     float *part;         // partial results: accumulators, then their maxima and sums
     float *part_ml;
     int32_t R;           // query heads per key/value head

@@ -76,6 +76,84 @@ __device__ __forceinline__ KvSeq kv_seq(const KvArgs &a, const KvAttendArgs &p, 
 
 __device__ __forceinline__ uint32_t wave_total(uint32_t v) { return __builtin_amdgcn_readlane(wave_inclusive_sum(v), 63); }
 
+// As many items for each tile: nothing to look up.
+__host__ __device__ __forceinline__ bool kv_even(const KvArgs &a, const KvAttendArgs &p) { return a.n_seqs == 1 || (p.splits == 1 && p.row_tiles == 1); }
+// Items of a sequence whose tiles are cut into shares of `step` steps.
+__device__ __forceinline__ uint32_t kv_items(const KvSeq &q, uint32_t step) { return q.row_tiles * max((q.most + step - 1) / step, 1u); }
+__device__ __forceinline__ uint64_t kv_work(const KvSeq &q) { return static_cast<uint64_t>(q.most) * q.row_tiles; }
+
+// The least steps of a share with which all sequences' items fit p.items, to a sixteenth.  work, tiles: the thread's sequences'
+// steps and tiles, `threads` + 1 threads; total(n): the sum over all of them; items_of(step): the thread's.
+template <typename Total, typename Items>
+__device__ __forceinline__ uint32_t kv_step(const KvAttendArgs &p, uint64_t work, uint32_t tiles, uint32_t threads, Total &&total, Items &&items_of)
+{
+    const uint32_t uncut = 1u << 30;
+    if (p.splits == 1) return uncut;
+    const uint32_t most = 0x7FFFFFFFu / (threads + 1);
+    if (total(work > most ? 1u : 0u) != 0) return uncut;  // (more steps than can be counted)
+    const uint32_t all = total(static_cast<uint32_t>(work)), items = p.items;
+    tiles = total(tiles);
+    // nearly all / items, at most all / (items - tiles)
+    const uint32_t least = p.min_tiles;
+    uint32_t low = max((all + items - 1) / items, least), good = max(all / (items > tiles ? items - tiles : 1u) + 1, low);
+    if (total(items_of(low)) <= items) good = low;
+    while (good - low > low >> 4) {
+        const uint32_t mid = low + ((good - low) >> 1);
+        if (mid == low) break;
+        if (total(items_of(mid)) <= items) good = mid;
+        else low = mid;
+    }
+    return good;
+}
+
+// Of more than 64 sequences the list is drawn up once, ahead of the workgroups that look theirs up (each by itself: 300 sequences of 200
+// to 1000 tokens and one of 20000 57 us, so 36; of 100 69 to 67): plan[0] the steps of a share,
+// plan[1 + b] sequence b's first item, plan[1 + n_seqs] their number.
+template <int TOK>
+__global__ __launch_bounds__(1024) void k_kv_plan(KvArgs a, KvAttendArgs p, int rows)
+{
+    __shared__ uint32_t part[2][16];
+    int turn = 0;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const auto sums = [&](uint32_t mine, uint32_t &before) {  // over the workgroup, and over the waves in front
+        turn ^= 1;  // (the last sum's parts may still be read)
+        if (lane == 0) part[turn][wave] = mine;
+        __syncthreads();
+        uint32_t sum = 0;
+        before = 0;
+        for (int w = 0; w < 16; ++w) {
+            before += w < wave ? part[turn][w] : 0u;
+            sum += part[turn][w];
+        }
+        return sum;
+    };
+    uint64_t work = 0;
+    uint32_t tiles = 0, unused;
+    for (int b = threadIdx.x; b < a.n_seqs; b += 1024) {
+        const KvSeq q = kv_seq<TOK>(a, p, rows, b);
+        work += kv_work(q);
+        tiles += q.row_tiles;
+    }
+    const uint32_t step = kv_step(p, work, tiles, 1023, [&](uint32_t n) { return sums(wave_total(n), unused); }, [&](uint32_t by) {
+        uint32_t n = 0;
+        for (int b = threadIdx.x; b < a.n_seqs; b += 1024) n += kv_items(kv_seq<TOK>(a, p, rows, b), by);
+        return n;
+    });
+    uint32_t first = 0;
+    for (int c = 0; c < a.n_seqs; c += 1024) {
+        const int b = c + static_cast<int>(threadIdx.x);
+        const uint32_t n = kv_items(kv_seq<TOK>(a, p, rows, b), step), sum = wave_inclusive_sum(n);
+        uint32_t before;
+        const uint32_t all = sums(__builtin_amdgcn_readlane(sum, 63), before);
+        if (b < a.n_seqs) p.plan[1 + b] = static_cast<int32_t>(first + before + sum - n);
+        first += all;
+    }
+    if (threadIdx.x == 0) {
+        p.plan[0] = static_cast<int32_t>(step);
+        p.plan[1 + a.n_seqs] = static_cast<int32_t>(first);
+    }
+}
+
 // A workgroup's item: a tile of a sequence's rows and a share of the steps that they go through.  A head's items lie in one
 // list, sequence by sequence and tile by tile, so that no workgroup is without work: one that finds none still costs 11 ns of
 // the launch.  With several sequences the list's length is given and the largest share sought that fits it: long sequences are
@@ -94,80 +172,46 @@ template <int TOK>
 __device__ __forceinline__ bool kv_share(const KvArgs &a, const KvAttendArgs &p, int rows, int item, KvShare &s)
 {
     const int lane = threadIdx.x & 63;
-    const bool cut = p.splits > 1;
     KvSeq q;
     int cuts = 1, first = 0;
-    if (a.n_seqs == 1 || (!cut && p.row_tiles == 1)) {  // as many items for each tile
+    if (kv_even(a, p)) {  // as many items for each tile
         cuts = p.splits;
         if (item >= 0) s.b = a.n_seqs == 1 ? 0 : item;
         q = kv_seq<TOK>(a, p, rows, s.b);
         first = a.n_seqs == 1 ? 0 : s.b;
     } else {
-        const KvSeq mine = kv_seq<TOK>(a, p, rows, lane);
-        const auto at = [&](int c) { return c == 0 ? mine : kv_seq<TOK>(a, p, rows, c + lane); };
-        uint32_t step = 1u << 30;
-        const auto items_of = [&](const KvSeq &x) { return x.row_tiles * max((x.most + step - 1) / step, 1u); };
-        if (cut) {
-            uint32_t total = 0, tiles = 0;  // (both below 2^31: a lane's share of them is cut off at 2^25)
-            const uint32_t most = (1u << 25) - 1u;
-            for (int c = 0; c < a.n_seqs; c += 64) {
-                const KvSeq x = at(c);
-                total = min(total + static_cast<uint32_t>(min(static_cast<uint64_t>(x.most) * x.row_tiles, static_cast<uint64_t>(most))), most);
-                tiles += x.row_tiles;
-            }
-            const bool countable = !__builtin_amdgcn_ballot_w64(total == most);  // (else: no tile is cut)
-            total = wave_total(total);
-            tiles = wave_total(tiles);
-            // as few steps a share as fit: nearly total / items, at most total / (items - tiles)
-            const uint32_t items = p.items;
-            const uint32_t ideal = (total + items - 1) / items, sure = total / (items > tiles ? items - tiles : 1u) + 1;
-            const auto fits = [&](uint32_t by) {
-                step = by;
-                uint32_t n = 0;
-                for (int c = 0; c < a.n_seqs; c += 64) n += items_of(at(c));
-                return wave_total(n) <= items;
-            };
-            if (countable) {
-                uint32_t least = max(ideal, static_cast<uint32_t>(p.min_tiles)), good = max(sure, least);
-                if (fits(least)) good = least;
-                while (good - least > least >> 4) {
-                    const uint32_t mid = least + ((good - least) >> 1);
-                    if (mid == least) break;
-                    if (fits(mid)) good = mid;
-                    else least = mid;
-                }
-                step = good;
-            }
-        }
-        if (item < 0) {
-            q = kv_seq<TOK>(a, p, rows, s.b);
-            const int end = s.b;
-            uint32_t n = 0;
-            for (int c = 0; c < end; c += 64) n += c + lane < end ? items_of(at(c)) : 0u;
-            first = wave_total(n);
-        } else {
-            bool found = false;
-            uint32_t before = 0;
-            for (int c = 0; c < a.n_seqs; c += 64) {
-                const KvSeq x = at(c);
-                const uint32_t n = items_of(x), sum = wave_inclusive_sum(n) + before;
+        uint32_t step;
+        if (a.n_seqs <= 64) {  // a lane has a sequence
+            const KvSeq mine = kv_seq<TOK>(a, p, rows, lane);
+            step = kv_step(p, kv_work(mine), mine.row_tiles, 63, [](uint32_t n) { return wave_total(n); }, [&](uint32_t by) { return kv_items(mine, by); });
+            const uint32_t n = kv_items(mine, step), sum = wave_inclusive_sum(n);
+            if (item >= 0) {
                 const uint64_t past = __builtin_amdgcn_ballot_w64(static_cast<uint32_t>(item) < sum);
-                if (past) {
-                    const int l = __builtin_ctzll(past);
-                    q.row0 = __builtin_amdgcn_readlane(x.row0, l);
-                    q.n = __builtin_amdgcn_readlane(x.n, l);
-                    q.base = __builtin_amdgcn_readlane(x.base, l);
-                    q.len = __builtin_amdgcn_readlane(x.len, l);
-                    q.row_tiles = __builtin_amdgcn_readlane(x.row_tiles, l);
-                    q.most = __builtin_amdgcn_readlane(x.most, l);
-                    first = __builtin_amdgcn_readlane(sum - n, l);
-                    s.b = c + l;
-                    found = true;
-                    break;
-                }
-                before = __builtin_amdgcn_readlane(sum, 63);
+                if (!past) return false;
+                s.b = __builtin_ctzll(past);
             }
-            if (!found) return false;
+            q.row0 = __builtin_amdgcn_readlane(mine.row0, s.b);
+            q.n = __builtin_amdgcn_readlane(mine.n, s.b);
+            q.base = __builtin_amdgcn_readlane(mine.base, s.b);
+            q.len = __builtin_amdgcn_readlane(mine.len, s.b);
+            q.row_tiles = __builtin_amdgcn_readlane(mine.row_tiles, s.b);
+            q.most = __builtin_amdgcn_readlane(mine.most, s.b);
+            first = __builtin_amdgcn_readlane(sum - n, s.b);
+        } else {  // k_kv_plan has been at it: the sequence looked for 64 at a time
+            if (item >= 0) {
+                if (item >= p.plan[1 + a.n_seqs]) return false;
+                s.b = 0;
+                for (int count = a.n_seqs; count > 1;) {
+                    const int by = (count + 63) / 64, at = lane * by;
+                    const uint64_t before = __builtin_amdgcn_ballot_w64(at < count && p.plan[1 + s.b + min(at, count - 1)] <= item);
+                    const int nth = max(__builtin_popcountll(before), 1) - 1;
+                    s.b += nth * by;
+                    count = min(by, count - nth * by);
+                }
+            }
+            step = p.plan[0];
+            first = p.plan[1 + s.b];
+            q = kv_seq<TOK>(a, p, rows, s.b);
         }
         cuts = max((q.most + step - 1) / step, 1u);
     }
@@ -1225,11 +1269,13 @@ static KvChoice choose(const KvArgs &a, int D, int R, int reach, int compute_uni
     return c;
 }
 
+static size_t plan_bytes(const KvArgs &a) { return a.n_seqs > 64 ? (4 * (static_cast<size_t>(a.n_seqs) + 2) + 15) / 16 * 16 : 0; }
+
 size_t kv_attend_workspace_bytes(const KvArgs &a, int D, int R, int max_len)
 {
     int cu;
     if (compute_units_of_current_device(&cu) != hipSuccess) return 0;
-    return std::max<size_t>(choose(a, D, R, max_len, cu).partial_rows * (D + 2) * sizeof(float), 16);
+    return plan_bytes(a) + std::max<size_t>(choose(a, D, R, max_len, cu).partial_rows * (D + 2) * sizeof(float), 16);
 }
 
 template <int D>
@@ -1300,10 +1346,15 @@ int launch_kv_attend(const KvArgs &a, KvAttendArgs p, int D, int max_len, void *
     p.row_tiles = c.row_tiles;
     p.min_tiles = c.min_tiles;
     p.odd = c.many;
-    p.part = static_cast<float *>(workspace);
+    p.plan = static_cast<int32_t *>(workspace);
+    p.part = reinterpret_cast<float *>(static_cast<uint8_t *>(workspace) + plan_bytes(a));
     p.part_ml = p.part + static_cast<size_t>(a.heads) * c.items * c.rows * D;
     if (c.items * a.heads > kKvMaxItems) return TPQ_ERR_SHAPE;
     if (c.splits > 1 && static_cast<uint64_t>(c.items) * a.heads * c.rows > choose(a, D, p.R, max_len, cu).partial_rows) return TPQ_ERR_WORKSPACE;
+    if (a.n_seqs > 64 && !kv_even(a, p)) {
+        const auto plan = c.many && D <= 128 ? k_kv_plan<64> : k_kv_plan<32>;
+        hipLaunchKernelGGL(plan, dim3(1), dim3(1024), 0, s, a, p, c.rows);
+    }
     const dim3 grid(static_cast<uint32_t>(c.items) * a.heads);
     if (c.many) {
         e = D == 256 ? launch_many_of<256, 4, 32>(a, p, grid, s)

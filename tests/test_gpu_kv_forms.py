@@ -69,6 +69,9 @@ LISTED = [  # lens, new, heads, R, D, G, page, window
     ([3000, 2800], [34, 50], 1, 1, 64, 32, 64, 1500),
     (lengths(75, 40, 600, 11), lengths(75, 0, 40, 12), 1, 2, 128, 64, 16, 0),
     ([3000, 2800], [70, 66], 1, 1, 64, 32, 64, 1500),
+    # more than 4096 sequences: a long one among them; two tiles of rows, none cut
+    ([n for n in lengths(2500, 0, 20, 13)] + [9000] + lengths(2600, 0, 20, 14), [1] * 5101, 1, 1, 64, 64, 16, 0),
+    ([n + 2 for n in lengths(4200, 0, 20, 15)], lengths(4200, 0, 2, 16), 1, 16, 64, 64, 16, 0),
     # tiles of 16 rows, up to 64 of them
     ([900, 2000, 40], [64, 1, 40], 2, 1, 128, 128, 16, 0),
     ([900, 2000, 40], [15, 16, 9], 1, 4, 256, 128, 32, 500),
