@@ -129,3 +129,30 @@ def test_two_streams_at_once(new):
     torch.cuda.synchronize()
     for o in outs:
         assert torch.equal(o, want)
+
+
+@pytest.mark.parametrize("count,new,heads", [(70, 1, 8), (70, 3, 2), (3, 80, 2), (80, 70, 1), (1, 300, 2)])
+def test_captured_and_replayed_with_other_lengths(count, new, heads):
+    """The list of items, the shares and their sums follow lengths and starts that change between replays; eager work lies between."""
+    c = kv.Cache([1500 if b == 1 or count == 1 else 500 for b in range(count)], [new] * count, heads, 128, 128, 16, seed=count, width=1251).fill()
+    cache, batch = kv.dev(c.bytes), c.batch(single=new == 1, max_len=20000 if count == 70 else None)
+    Q = torch.randn((c.rows, 2 * heads, 128), device="cuda").to(torch.bfloat16)
+    out, want = torch.zeros_like(Q), torch.zeros_like(Q)
+    ws, ws2 = (tpq.kv_attention_workspace(c.L, batch, 2 * heads, "cuda") for _ in range(2))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        tpq.kv_attention(c.L, cache, batch, Q, out, 0.1, ws)
+    rng = np.random.default_rng(count + new)
+    for _ in range(5):
+        lens = [int(rng.integers(0, n + 1)) for n in c.lens]
+        mine = [int(min(n, rng.integers(0, new + 1))) for n in lens] if new > 1 else [1] * count
+        batch.lens.copy_(torch.tensor(lens, dtype=torch.int32))
+        if new > 1:
+            batch.starts.copy_(torch.tensor(np.concatenate(([0], np.cumsum(mine))), dtype=torch.int32))
+        out.fill_(3.0)
+        want.fill_(3.0)
+        tpq.kv_attention(c.L, cache, batch, Q, want, 0.1, ws2.fill_(kv.GARBAGE))
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want)
