@@ -435,6 +435,8 @@ int tpq_kv_read(const tpq_kv_layout *L, const void *cache, const tpq_kv_batch *b
  * With up to 64 rows of a head (max_new * q_heads / L.heads) per sequence, 32 where D = 4 G and 8 where
  * D = 8 G, the products take the codes themselves, which are exact in bf16, and the probabilities as
  * pairs of bf16 (17 bits); with more, keys and values are rounded to fp16 at a scale of their own and so are the probabilities (2^-12).
+ * max_new decides for the whole batch: single tokens beside long prompts are faster in a call of their
+ * own (63 of them over 2000 to 4000 tokens and 256 over 4000, 8 heads of 128: 183 us in one call, 61 + 41 in two).
  *     Q, out    [device] bf16 [rows][ldQ], [rows][ldOut], elements, multiples of 8
  *     window, sinks  >= 0, at most 2^28 (sinks without a window change nothing)
  *     workspace [device] >= tpq_kv_attention_workspace_bytes(..) bytes (which depends on L, the batch's
