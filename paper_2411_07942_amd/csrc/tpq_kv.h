@@ -28,10 +28,10 @@ struct KvDivisor {
         mul = static_cast<uint32_t>(((((1ull << lg) - by) << 32) / by) + 1);
         shift = lg - 1;
     }
-    __device__ __forceinline__ int of(int n) const  // n >= 0
+    __host__ __device__ __forceinline__ int of(int n) const  // n >= 0
     {
         if (d == 1) return n;
-        const uint32_t u = static_cast<uint32_t>(n), t = __umulhi(u, mul);
+        const uint32_t u = static_cast<uint32_t>(n), t = static_cast<uint32_t>((static_cast<uint64_t>(u) * mul) >> 32);
         return static_cast<int>((t + ((u - t) >> 1)) >> shift);
     }
 };
@@ -73,7 +73,7 @@ struct KvAttendArgs {
 };
 
 // A sequence's new rows and its length; false: its starts are no range of rows.
-__device__ __forceinline__ bool kv_sequence(const KvArgs &a, int b, int64_t &row0, int &n, int &len)
+__host__ __device__ __forceinline__ bool kv_sequence(const KvArgs &a, int b, int64_t &row0, int &n, int &len)
 {
     len = min(max(a.lens[b], 0), 1 << 30);
     row0 = b;
