@@ -224,7 +224,7 @@ __global__ __launch_bounds__(256, D <= 128 && (COLS || GROUPS <= 2) ? 3 : 2) voi
     if (!kv_share<kKvTile>(a, p, ROWS, item, w)) return;
     const int rt = w.rt, split = w.split, b = w.b;
     const int64_t row0 = w.row0;
-    const int n_rows = w.n_rows, base = w.base, len = w.len, lo = w.lo, hi = w.hi, live = w.live, share = w.share;
+    const int n_rows = w.n_rows, base = w.base, len = w.len, hi = w.hi, live = w.live, share = w.share;
     const KvSpan span = w.span;
     const int v1 = min((split + 1) * share, span.tiles);
 
@@ -251,6 +251,7 @@ __global__ __launch_bounds__(256, D <= 128 && (COLS || GROUPS <= 2) ? 3 : 2) voi
     }
 
     const int n_blocks = (min(len, a.ld_table << a.lg_page) + 15) / 16;  // blocks of 16 tokens that exist
+    const int all_to = min(w.lo, 16 * n_blocks - 1);                     // last token that every row may see (rows may lie past the table)
     const uint32_t page_len = 1u << a.lg_page, page_mask = page_len - 1u;
     const int32_t *table = a.table + static_cast<int64_t>(b) * a.ld_table;
     // The page numbers of the wave's next 32 steps, two a step, one a lane: one load's latency for all of them.
@@ -332,7 +333,7 @@ __global__ __launch_bounds__(256, D <= 128 && (COLS || GROUPS <= 2) ? 3 : 2) voi
 
     auto step = [&](const Raw &raw, int v) {
         const int t0 = span.tile(v) * kKvTile;
-        const bool whole = t0 + kKvTile - 1 <= lo && (p.window == 0 || t0 > hi - p.window || t0 + kKvTile <= p.sinks) && !raw.bad[0] && !raw.bad[1];
+        const bool whole = t0 + kKvTile - 1 <= all_to && (p.window == 0 || t0 > hi - p.window || t0 + kKvTile <= p.sinks) && !raw.bad[0] && !raw.bad[1];
         float s[2][4];
         bool vis[2][4];
         for_each<2>([&](auto jj) {
@@ -656,7 +657,7 @@ __global__ __launch_bounds__(64 * W, D == 256 ? 1 : 2) void k_kv_attend_many(KvA
     // 2^-3 .. 2^-2, so that scales fit fp16 times the codes' 2^20 (what is 2^12 times smaller than the largest still has
     // fp16's 11 bits, and then one less for every halving).  From scales and zeros alone, 8 ng bytes a token and head.
     float k_norm, v_norm, k_undo, v_undo;
-    bool absent;  // a block of 16 tokens that has no page
+    bool absent;  // a block of 16 tokens at or before some row has no page, or lies past the table
     {
         if (threadIdx.x < 3) reduced[threadIdx.x] = 0;
         uint32_t top[2] = {0, 0}, missing = 0;
@@ -666,7 +667,7 @@ __global__ __launch_bounds__(64 * W, D == 256 ? 1 : 2) void k_kv_attend_many(KvA
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const bool exists = key[u] < 16 * n_blocks, good = static_cast<uint32_t>(id[u]) < static_cast<uint64_t>(a.n_pages);
-                missing |= exists && !good ? 1u : 0u;
+                missing |= (!(exists & good) & (key[u] <= w.hi)) ? 1u : 0u;
                 const bool seen = exists & good & (key[u] <= w.hi) & ((p.window == 0) | (key[u] > w.lo - p.window) | (key[u] < p.sinks));
                 const uint32_t *src = reinterpret_cast<const uint32_t *>(cache_h + (good ? id[u] : 0) * a.page_bytes + page_len * D) + (static_cast<uint32_t>(key[u]) & page_mask);
 #pragma unroll
