@@ -1,5 +1,5 @@
 """Attention over the 4-bit cache with a window where a sequence's last tile of rows goes through fewer steps than an earlier one, and
-sequences are cut into shares."""
+sequences are cut into shares; and calls of 33 to 64 rows, or of 8 groups, at the bound of the kernel that they go to."""
 import pytest
 
 import kv_cases
@@ -36,3 +36,23 @@ def test_window_on_any_token_of_a_tile(over, new, R, window, sinks):
     kv_cases.attend(c, R, window=window, sinks=sinks)
     c = kv.Cache([4096 + over], [new], 1, 64, 32, 32, seed=over + new).fill()
     kv_cases.attend(c, R, window=window, sinks=sinks)
+
+
+RULE = [  # lens, new, heads, R, D, G, page, window, cap
+    ([33], [33], 1, 1, 128, 128, 16, 0, 0.0),
+    ([700, 40], [64, 40], 3, 1, 64, 64, 16, 0, 0.0),
+    ([3000, 2800], [34, 50], 1, 1, 64, 32, 64, 1500, 0.0),
+    ([900, 2000, 40], [15, 16, 9], 1, 4, 256, 128, 32, 500, 0.0),
+    ([900, 2000, 40], [64, 1, 40], 2, 1, 128, 128, 16, 0, 20.0),
+    ([500, 60], [4, 2], 2, 16, 128, 64, 16, 0, 0.0),
+    ([500, 60], [4, 2], 2, 8, 128, 32, 16, 0, 0.0),       # 32 rows of 4 groups
+    ([500, 60], [33, 2], 2, 1, 128, 32, 16, 0, 0.0),      # one more
+    ([500, 60], [2, 2], 2, 4, 256, 32, 16, 0, 0.0),       # 8 rows of 8 groups
+    ([500, 60], [3, 3], 2, 3, 256, 32, 16, 0, 0.0),       # one more
+]
+
+
+@pytest.mark.parametrize("lens,new,heads,R,D,G,page,window,cap", RULE)
+def test_rows_at_the_bound_of_their_kernel(lens, new, heads, R, D, G, page, window, cap):
+    c = kv.Cache(lens, new, heads, D, G, page, seed=sum(lens) + D).fill()
+    kv_cases.attend(c, R, window=window, cap=cap)
