@@ -367,6 +367,7 @@ int tpq_decode_reduce_static(const tpq_layout *L, const void *plan, int n_ranks,
  * tpq_kv_check reports all of these.  Matrices whose rows would take 2^32 threads or more are
  * refused (TPQ_ERR_SHAPE). */
 #define TPQ_KV_MAX_HEADS 256
+#define TPQ_KV_MAX_SOFTCAP 1024.0f
 
 typedef struct tpq_kv_layout {
     int32_t heads;      /* key/value heads on this device, 1 .. TPQ_KV_MAX_HEADS        */
@@ -429,9 +430,10 @@ int tpq_kv_read(const tpq_kv_layout *L, const void *cache, const tpq_kv_batch *b
 /* Attention of the batch's new tokens over the cache (which holds them already).  Query head
  * hq of q_heads (a multiple of L.heads) goes with key/value head hq / (q_heads / L.heads).  The
  * token at position p sees key j iff j <= p and (window = 0 or j > p - window or j < sinks):
- *     s_j = scale * q . k_j;  softcap > 0: s_j = softcap * tanh(s_j / softcap)
+ *     s_j = scale * q . k_j;  softcap > 0 (2^-20 .. 1024): s_j = softcap * tanh(s_j / softcap)
  *     out = sum_j exp(s_j) v_j / sum_j exp(s_j)        over the keys it sees; none: 0
- * with k_j, v_j the cache's values.  Scores, exponentials' sums and accumulators are fp32.
+ * with k_j, v_j the cache's values.  Scores, exponentials' sums and accumulators are fp32; a bounded score is off by up to
+ * 2^-22 softcap, so that larger bounds are refused (TPQ_ERR_SHAPE): what is meant to bound nothing is 0.
  * With up to 64 rows of a head (max_new * q_heads / L.heads) per sequence, 32 where D = 4 G and 8 where
  * D = 8 G, the products take the codes themselves, which are exact in bf16, and the probabilities as
  * pairs of bf16 (17 bits); with more, keys and values are rounded to fp16 at a scale of their own and so are the probabilities (2^-12).

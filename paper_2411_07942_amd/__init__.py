@@ -512,5 +512,6 @@ def kv_attention_call(L: KvLayout, cache: torch.Tensor, batch: KvBatch, Q: torch
 def kv_attention(L: KvLayout, cache: torch.Tensor, batch: KvBatch, Q: torch.Tensor, out: torch.Tensor, scale: float,
                  workspace: torch.Tensor, window: int = 0, sinks: int = 0, softcap: float = 0.0, stream=None) -> None:
     """out = softmax(scale * Q K^T) V of the batch's new tokens over the cache; Q, out bf16 [rows, q_heads, D].  A token
-    sees the keys up to its own, of those (window > 0) the last `window` and the first `sinks`."""
+    sees the keys up to its own, of those (window > 0) the last `window` and the first `sinks`.  softcap: scores are bounded by it
+    (softcap * tanh(score / softcap); 2^-20 .. 1024, 0: not at all)."""
     _native().kv_attention(L, cache, batch, Q, out, scale, workspace, window, sinks, softcap, stream)

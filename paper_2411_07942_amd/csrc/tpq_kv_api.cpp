@@ -183,7 +183,9 @@ int tpq_kv_attention(const tpq_kv_layout *L, const void *cache, const tpq_kv_bat
     if (bad_query_heads(L, q_heads)) return TPQ_ERR_SHAPE;
     const int64_t Eq = static_cast<int64_t>(q_heads) * L->D;
     if (ldQ < Eq || ldOut < Eq || window < 0 || window > 1 << 28 || sinks < 0 || sinks > 1 << 28) return TPQ_ERR_SHAPE;
-    if (!isfinite(scale) || !isfinite(softcap) || softcap < 0.0f) return TPQ_ERR_SHAPE;
+    if (!isfinite(scale) || !isfinite(softcap)) return TPQ_ERR_SHAPE;
+    // (a bounded score is off by 2^-22 of the bound, whatever its size; 1 / softcap times a score stays finite)
+    if (softcap != 0.0f && !(softcap >= 0x1p-20f && softcap <= TPQ_KV_MAX_SOFTCAP)) return TPQ_ERR_SHAPE;
     if ((ldQ % 8) != 0 || (ldOut % 8) != 0) return TPQ_ERR_ALIGN;
     if (batch->rows == 0) return TPQ_OK;
     if (!cache || !Q || !out || !workspace) return TPQ_ERR_NULL;
