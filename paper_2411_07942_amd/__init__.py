@@ -432,7 +432,14 @@ class KvBatch:
     """Where a batch's sequences lie (tpq_kv_batch): table int32 [n_seqs, entries], page numbers; lens int32
     [n_seqs], tokens in the cache with the new ones; starts int32 [n_seqs + 1], the rows of each sequence's new tokens, or
     None: one new token per sequence, row b for sequence b.  max_new: no sequence has more new tokens; max_len: no
-    sequence is expected to be longer (None: the whole table).  The tensors are read at each call, on the device."""
+    sequence is expected to be longer (None: the whole table).  The tensors are read at each call, on the device: their
+    contents may change, the batch itself is what it was made of (it keeps the tensors as long as a call may read them)."""
+
+    table = property(lambda self: self._tensors[0])
+    lens = property(lambda self: self._tensors[1])
+    starts = property(lambda self: self._tensors[2])
+    max_new = property(lambda self: self._c.max_new)
+    max_len = property(lambda self: self._c.max_len or None)
 
     def __init__(self, table: torch.Tensor, lens: torch.Tensor, starts: Optional[torch.Tensor] = None, max_new: int = 1,
                  max_len: Optional[int] = None):
@@ -448,8 +455,7 @@ class KvBatch:
             raise AssertionError("starts is a contiguous [n_seqs + 1]")
         if max_new < 1 or (max_len is not None and max_len < 1):
             raise AssertionError("max_new and max_len are at least 1")
-        self.table, self.lens, self.starts = table, lens, starts
-        self.max_new, self.max_len = int(max_new), max_len
+        self._tensors = (table, lens, starts)
         self._c = _KvBatch(table.data_ptr(), lens.data_ptr(), None if starts is None else starts.data_ptr(), n,
                            table.shape[1], int(max_new), 0 if max_len is None else int(max_len), 0, 0, table.device.index)
 

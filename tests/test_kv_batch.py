@@ -1,0 +1,40 @@
+"""KvBatch without a GPU: stand-ins for tensors on one, whose addresses nobody follows."""
+import gc
+import weakref
+
+import pytest
+import torch
+
+import paper_2411_07942_amd as tpq
+
+
+class OnGpu:
+    dtype, is_cuda, device = torch.int32, True, torch.device("cuda", 0)
+
+    def __init__(self, *shape):
+        self.shape = torch.Size(shape)
+
+    def dim(self):
+        return len(self.shape)
+
+    def is_contiguous(self):
+        return True
+
+    def data_ptr(self):
+        return id(self)
+
+
+def test_a_batch_is_what_it_was_made_of():
+    """Calls take the addresses that it was made with: another tensor in its place would not be read, and the first one's memory
+    would be someone else's."""
+    table, lens, starts = OnGpu(2, 3), OnGpu(2), OnGpu(3)
+    batch = tpq.KvBatch(table, lens, starts, max_new=5, max_len=40)
+    assert (batch.table, batch.lens, batch.starts, batch.max_new, batch.max_len) == (table, lens, starts, 5, 40)
+    for name, value in (("table", OnGpu(2, 3)), ("lens", OnGpu(2)), ("starts", None), ("max_new", 6), ("max_len", None)):
+        with pytest.raises(AttributeError):
+            setattr(batch, name, value)
+    alive = [weakref.ref(t) for t in (table, lens, starts)]
+    del table, lens, starts
+    gc.collect()
+    assert all(r() is not None for r in alive)
+    assert tpq.KvBatch(OnGpu(2, 3), OnGpu(2)).max_len is None
