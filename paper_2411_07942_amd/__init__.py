@@ -453,8 +453,8 @@ class KvBatch:
             raise AssertionError("lens is a contiguous [n_seqs]")
         if starts is not None and (starts.shape != (n + 1,) or not starts.is_contiguous()):
             raise AssertionError("starts is a contiguous [n_seqs + 1]")
-        if max_new < 1 or (max_len is not None and max_len < 1):
-            raise AssertionError("max_new and max_len are at least 1")
+        if not 1 <= max_new <= 0x7FFFFFFF or not (max_len is None or 1 <= max_len <= 0x7FFFFFFF):
+            raise AssertionError("max_new and max_len are at least 1 and at most 2^31 - 1")
         self._tensors = (table, lens, starts)
         self._c = _KvBatch(table.data_ptr(), lens.data_ptr(), None if starts is None else starts.data_ptr(), n,
                            table.shape[1], int(max_new), 0 if max_len is None else int(max_len), 0, 0, table.device.index)

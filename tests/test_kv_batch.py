@@ -38,3 +38,10 @@ def test_a_batch_is_what_it_was_made_of():
     gc.collect()
     assert all(r() is not None for r in alive)
     assert tpq.KvBatch(OnGpu(2, 3), OnGpu(2)).max_len is None
+
+
+@pytest.mark.parametrize("max_new,max_len", [(0, None), (-1, None), (1 << 31, None), ((1 << 32) + 1, None), (1, 0), (1, -5), (1, 1 << 32), (1, (1 << 32) + 7)])
+def test_numbers_that_no_call_takes(max_new, max_len):
+    """(cut to 32 bits, 2^32 + 1 new tokens would have been 1, and the others left out)"""
+    with pytest.raises(AssertionError):
+        tpq.KvBatch(OnGpu(2, 3), OnGpu(2), OnGpu(3), max_new, max_len)
