@@ -468,6 +468,8 @@ class KvBatch:
 
 def kv_check(L: KvLayout, cache: torch.Tensor, batch: KvBatch, rows: int, stream=None) -> None:
     """Waits for the stream and raises where the batch (whose matrices have `rows` rows) does not fit (tpq_kv_check)."""
+    if not cache.is_cuda or cache.device.index != batch._c.device or torch.cuda.current_device() != batch._c.device:
+        raise AssertionError("the cache and the batch's tensors are on the current device")
     c = batch._for(L, rows, cache.numel() * cache.element_size() // L.page_bytes)
     _check(_load().tpq_kv_check(ctypes.byref(L), ctypes.byref(c), _stream(stream)), "tpq_kv_check")
 

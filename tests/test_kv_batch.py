@@ -45,3 +45,20 @@ def test_numbers_that_no_call_takes(max_new, max_len):
     """(cut to 32 bits, 2^32 + 1 new tokens would have been 1, and the others left out)"""
     with pytest.raises(AssertionError):
         tpq.KvBatch(OnGpu(2, 3), OnGpu(2), OnGpu(3), max_new, max_len)
+
+
+def test_check_of_another_device(monkeypatch):
+    """As the other calls: the stream that is waited for is the current device's, and says nothing of another one's work."""
+    L = tpq.kv_layout_init(1, 64, 64, 16)
+    monkeypatch.setattr(tpq, "_load", lambda: pytest.fail("not refused"))
+    batch = tpq.KvBatch(OnGpu(2, 3), OnGpu(2))
+    with pytest.raises(AssertionError):
+        tpq.kv_check(L, torch.zeros(4 * L.page_bytes, dtype=torch.uint8), batch, 2)      # not on a GPU
+    cache = OnGpu(4 * L.page_bytes)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    with pytest.raises(AssertionError):
+        tpq.kv_check(L, cache, batch, 2)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    cache.device = torch.device("cuda", 1)
+    with pytest.raises(AssertionError):
+        tpq.kv_check(L, cache, batch, 2)
