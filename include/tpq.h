@@ -434,6 +434,8 @@ int tpq_kv_read(const tpq_kv_layout *L, const void *cache, const tpq_kv_batch *b
  *     out = sum_j exp(s_j) v_j / sum_j exp(s_j)        over the keys it sees; none: 0
  * with k_j, v_j the cache's values.  Scores, exponentials' sums and accumulators are fp32; a bounded score is off by up to
  * 2^-22 softcap, so that larger bounds are refused (TPQ_ERR_SHAPE): what is meant to bound nothing is 0.
+ * Cached values go up to 2^80 and scores (scale * q . k, before a bound) up to 2^24 in magnitude, where fp32 scores are whole
+ * numbers; beyond, outputs may be anything, NaN too (from scores of 2^28 and values of 2^85 on).
  * With up to 64 rows of a head (max_new * q_heads / L.heads) per sequence, 32 where D = 4 G and 8 where
  * D = 8 G, the products take the codes themselves, which are exact in bf16, and the probabilities as
  * pairs of bf16 (17 bits); with more, keys and values are rounded to fp16 at a scale of their own and so are the probabilities (2^-12).
