@@ -56,6 +56,7 @@ struct KvReadArgs {
     KvDivisor by_columns;
 };
 
+// (In this order: with window and scale in front of the numbers that a workgroup finds its item by, a call took 0.2 us longer: one token of 5 heads over 641 9.3, so 9.15.)
 struct KvAttendArgs {
     const uint8_t *Q;
     uint8_t *out;
@@ -63,13 +64,13 @@ struct KvAttendArgs {
     int32_t *plan;       // the list of items, of more than 64 sequences
     float *part;         // partial results: accumulators, then their maxima and sums
     float *part_ml;
-    int32_t R;           // query heads per key/value head
-    KvDivisor by_R, by_rows, by_heads, by_splits;  // (rows: of a tile)
-    int32_t window, sinks;
-    float scale, softcap;
+    int32_t R;                          // query heads per key/value head
+    KvDivisor by_R, by_rows, by_heads;  // (rows: of a tile)
     int32_t splits;      // 1: no tile of rows is cut; with one sequence: shares of a tile's steps
     int32_t odd;         // 1: shares of an odd number of steps
     int32_t items, row_tiles, min_tiles;  // items of a head, most tiles of rows of a sequence, least steps of a share
+    int32_t window, sinks;
+    float scale, softcap;
 };
 
 // A sequence's new rows and its length; false: its starts are no range of rows.

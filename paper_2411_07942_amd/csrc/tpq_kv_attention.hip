@@ -14,7 +14,7 @@
 //
 // Many rows are bound by products, and every key meets 128 or 256 of them: tiles of 64 tokens are dequantised once, to fp16, into
 // LDS for 4 or 8 waves of 32 rows, products are 32 x 32 x 16.  (4096 tokens over 16384, 32 heads: 0.98 ms, 980 TFLOP/s; matrix
-// cores busy 49 % and the vector unit 55 % of the time, at 1.9 GHz.)
+// cores busy 48 % and the vector unit 55 % of the time, at 1.9 GHz.)
 #include <atomic>
 #include <type_traits>
 #include <utility>
@@ -1057,10 +1057,9 @@ __global__ __launch_bounds__(64 * W, D == 256 ? 1 : 2) void k_kv_attend_many(KvA
     }
 }
 
-// The splits' results into the output: a row of a head by D / 4 lanes.  Every split's maximum and sum first, then the
-// accumulators, eight splits' loads at a time: one after the other they would be as many latencies (43 splits: 22.8 us).
-// The shares of a row put together: D / 4 lanes a row, 8 shares' loads at a time (32 shares of 24 rows of 128: 7 us, most of
-// it the way to the first load).
+// The shares of a row put together: D / 4 lanes a row, 8 shares' maxima, sums and accumulators in flight at a time (32 shares of
+// 24 rows of 128: 7 us, most of it the way to the first load).  The grid has every row that the batch may have; those that were not cut
+// return once their share is known.
 template <int D, int TOK>
 __global__ __launch_bounds__(256) void k_kv_join(KvArgs a, KvAttendArgs p, int rows)
 {

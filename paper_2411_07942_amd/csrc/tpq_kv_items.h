@@ -191,7 +191,6 @@ inline void take_choice(const KvArgs &a, const KvChoice &c, KvAttendArgs &p)
 {
     p.splits = c.splits;
     p.by_R = KvDivisor(p.R);
-    p.by_splits = KvDivisor(c.splits);
     p.by_heads = KvDivisor(a.heads);
     p.by_rows = KvDivisor(c.rows);
     p.items = c.items;
