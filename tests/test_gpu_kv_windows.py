@@ -1,8 +1,11 @@
 """Attention over the 4-bit cache with a window where a sequence's last tile of rows goes through fewer steps than an earlier one, and
 sequences are cut into shares; and calls of 33 to 64 rows, or of 8 groups, at the bound of the kernel that they go to."""
+import numpy as np
 import pytest
+import torch
 
 import kv_cases
+import paper_2411_07942_amd as tpq
 import test_gpu_kv as kv
 
 pytestmark = pytest.mark.gpu
@@ -56,3 +59,31 @@ RULE = [  # lens, new, heads, R, D, G, page, window, cap
 def test_rows_at_the_bound_of_their_kernel(lens, new, heads, R, D, G, page, window, cap):
     c = kv.Cache(lens, new, heads, D, G, page, seed=sum(lens) + D).fill()
     kv_cases.attend(c, R, window=window, cap=cap)
+
+
+@pytest.mark.parametrize("count,new,heads,R", [(1, 9, 2, 2), (4, 9, 2, 2), (70, 9, 1, 2), (1, 140, 2, 1), (5, 140, 1, 2)])
+def test_captured_windows_follow_the_lengths(count, new, heads, R):
+    """A captured call over cut, windowed tiles, replayed with other lengths and starts, its workspace full of NaN; eager work between."""
+    c = kv.Cache([4000 if b == 0 else 2500 for b in range(count)], [new] * count, heads, 128, 128, 16, seed=count).fill()
+    cache, batch = kv.dev(c.bytes), c.batch()
+    Q = torch.randn((c.rows, R * heads, 128), device="cuda").to(torch.bfloat16)
+    out, want = torch.zeros_like(Q), torch.zeros_like(Q)
+    ws, ws2 = (tpq.kv_attention_workspace(c.L, batch, R * heads, "cuda") for _ in range(2))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        tpq.kv_attention(c.L, cache, batch, Q, out, 0.1, ws, 1000, 3)
+    rng = np.random.default_rng(count + new)
+    for _ in range(5):
+        lens = [int(rng.integers(0, n + 1)) for n in c.lens]
+        mine = [int(min(n, rng.integers(0, new + 1))) for n in lens]
+        batch.lens.copy_(torch.tensor(lens, dtype=torch.int32))
+        batch.starts.copy_(torch.tensor(np.concatenate(([0], np.cumsum(mine))), dtype=torch.int32))
+        out.fill_(3.0)
+        want.fill_(3.0)
+        tpq.kv_attention(c.L, cache, batch, Q, want, 0.1, ws2.fill_(kv.GARBAGE), 1000, 3)
+        ws.fill_(kv.GARBAGE)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want) and torch.isfinite(want.float()).all()
+        assert (out[sum(mine):] == 3.0).all()
