@@ -434,11 +434,11 @@ int tpq_kv_read(const tpq_kv_layout *L, const void *cache, const tpq_kv_batch *b
  *     out = sum_j exp(s_j) v_j / sum_j exp(s_j)        over the keys it sees; none: 0
  * with k_j, v_j the cache's values.  Scores, exponentials' sums and accumulators are fp32; a bounded score is off by up to
  * 2^-22 softcap, so that larger bounds are refused (TPQ_ERR_SHAPE): what is meant to bound nothing is 0.
- * Cached values go up to 2^80 and scores (scale * q . k, before a bound) up to 2^24 in magnitude, where fp32 scores are whole
+ * Cached values go up to 2^80 and scores that have no bound up to 2^24 in magnitude, where fp32 scores are whole
  * numbers; beyond, outputs may be anything, NaN too (from scores of 2^28 and values of 2^85 on).
  * With up to 64 rows of a head (max_new * q_heads / L.heads) per sequence, 32 where D = 4 G and 8 where
  * D = 8 G, the products take the codes themselves, which are exact in bf16, and the probabilities as
- * pairs of bf16 (17 bits); with more, keys and values are rounded to fp16 at a scale of their own and so are the probabilities (2^-12).
+ * pairs of bf16 (17 bits); with more, keys and values are rounded to fp16 at a scale of their own and so are the probabilities (2^-11 each).
  * max_new decides for the whole batch: single tokens beside long prompts are faster in a call of their
  * own (63 of them over 2000 to 4000 tokens and 256 over 4000, 8 heads of 128: 183 us in one call, 61 + 41 in two).
  *     Q, out    [device] bf16 [rows][ldQ], [rows][ldOut], elements, multiples of 8
